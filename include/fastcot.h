@@ -288,6 +288,96 @@ int fastcot_attn_window_noalloc(const float* d_q, const void* d_k_cache, const v
                                 int32_t H, int32_t Hkv, int32_t Dh, int32_t max_seq, int32_t dtype, float* d_out,
                                 void* hip_stream);
 
+/* ------------------------------------------------------------------ a K/V cache in pages
+ * For serving loops whose sequences join, leave, are continued several times or grow past any fixed length: K and V of all
+ * sequences live in pages of page_size positions, and a table says which page holds which positions of a sequence.  The
+ * committed length n, the rows of a pass at positions n.. and the commit by raising n are those of a context's own cache (Sec. 4.3
+ * "Cache Update"); everything about the pages lives in device memory, so calls take no lengths from the host and may be
+ * captured into a graph.
+ *
+ * A pool (one for K, one for V) is [n_layers][n_pages][n_kv_heads][page_size / 32][32 * head_dim] elements of dtype: the blocks of
+ * 32 positions of fastcot_kv_scatter's layout.  page_size: a power of two, 32 to 4096; head_dim: 32, 64, 96, 128, 192 or 256;
+ * n_pages up to 2^24, max_seqs up to 4096, max_pages * page_size up to 2^30.
+ * table [max_seqs][max_pages]: page of positions i * page_size.. of a sequence, -1: none (no row sees those positions, and nothing is written
+ * there).  len [max_seqs]: committed positions.  ref [n_pages]: sequences whose table names the page, 0: free.
+ * All device memory is the caller's: pools (fastcot_paged_pool_bytes each, aligned to 16 bytes, contents arbitrary), table, len, ref (set by
+ * fastcot_paged_reset, changed by the calls below alone; a table entry outside 0..n_pages - 1 counts as none).
+ * d_scratch: fastcot_paged_scratch_bytes bytes, aligned to 256, zeroed once by the caller.  Calls that share a scratch must not overlap in time; neither
+ * may calls on one cache, except several fastcot_paged_attn with scratches of their own.  Nothing is allocated; nothing is kept on the host.
+ * Calls return 0, FASTCOT_EINVAL, FASTCOT_ECAPACITY or FASTCOT_EHIP with a text in fastcot_last_error(NULL); what only the device knows (a
+ * sequence number out of range, no free page) comes back in d_status, where given: one fastcot_status per entry of the call. */
+typedef struct fastcot_paged {
+    int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim;
+    int32_t dtype; /* of the cached values: FASTCOT_F32 or FASTCOT_BF16 */
+    int32_t max_seqs, max_pages;
+    void* k_pool; /* device */
+    void* v_pool;
+    int32_t* table;
+    int32_t* len;
+    int32_t* ref;
+} fastcot_paged;
+/* (sizes look at the numbers alone; 0 on invalid ones) */
+size_t fastcot_paged_pool_bytes(const fastcot_paged* cache);
+size_t fastcot_paged_scratch_bytes(const fastcot_paged* cache);
+/* Every sequence empty, every page free. */
+int fastcot_paged_reset(const fastcot_paged* cache, void* hip_stream);
+
+/* Bookkeeping of `count` entries (count <= max_seqs); d_seqs and the other arrays: device int32, one per entry.  An entry out of range gets
+ * FASTCOT_EINVAL in d_status (nullable) and changes nothing, and so does, except in free and trim, one that names a sequence an
+ * earlier entry named.  Results do not depend on timing.
+ * grow: pages for positions len .. len + rows - 1 that have none (before a pass writes them).  Entries get the lowest free pages in
+ *   the order of the call, a sequence's positions in ascending order; from the first entry on that the free pages do not suffice for, entries
+ *   that need any get FASTCOT_ECAPACITY and none, as does one whose positions pass max_pages * page_size.
+ * advance: len += rows (the commit of accepted rows); FASTCOT_ECAPACITY where those positions have no pages.
+ * fork: sequence dst, which has to be empty and not a source of this call, continues src: it shares the pages that src has filled and
+ *   gets a page of its own (the lowest free ones in the order of the call) with a copy of src's last page where that is partly filled: of the blocks
+ *   of 32 positions that hold any.  FASTCOT_ECAPACITY without a free page.
+ * trim: pages no later row sees under a sliding window (see fastcot_paged_attn) leave the sequence: those of positions >= sinks and
+ *   <= len - window.  window >= 1.
+ * free: every page leaves the sequence, len = 0.
+ * A page that no sequence names any more is free; its contents stay as they are. */
+int fastcot_paged_grow(const fastcot_paged* cache, int32_t count, const int32_t* d_seqs, const int32_t* d_rows, int32_t* d_status,
+                       void* d_scratch, void* hip_stream);
+int fastcot_paged_advance(const fastcot_paged* cache, int32_t count, const int32_t* d_seqs, const int32_t* d_rows, int32_t* d_status,
+                          void* hip_stream);
+int fastcot_paged_fork(const fastcot_paged* cache, int32_t count, const int32_t* d_src, const int32_t* d_dst, int32_t* d_status,
+                       void* d_scratch, void* hip_stream);
+int fastcot_paged_trim(const fastcot_paged* cache, int32_t count, const int32_t* d_seqs, int32_t window, int32_t sinks, int32_t* d_status,
+                       void* hip_stream);
+int fastcot_paged_free(const fastcot_paged* cache, int32_t count, const int32_t* d_seqs, int32_t* d_status, void* hip_stream);
+/* Moves the pages in use to the front of the pools: of U pages in use the i-th one (in ascending order) behind the first U places moves to the i-th
+ * free place among them, and the tables follow.  d_used (device, nullable): U.  Afterwards a caller may give the rear of the pools back or
+ * go on with a smaller n_pages (at least U). */
+int fastcot_paged_compact(const fastcot_paged* cache, int32_t* d_used, void* d_scratch, void* hip_stream);
+
+/* The rows of a pass.  d_seqs: device, n_seqs sequence numbers, NULL: 0 .. n_seqs - 1 (a number out of range: its rows see nothing and are not
+ * written).  d_row_start NULL: `rows` rows for each, sequence i's at i * rows, n_rows = n_seqs * rows.  Otherwise device, n_seqs + 1 entries
+ * ascending from 0 on up to at most n_rows: sequence i's rows are d_row_start[i] .. d_row_start[i + 1] - 1 (of which at most `rows`
+ * are used).  Row j of a sequence stands at position len + j. */
+typedef struct fastcot_paged_rows {
+    int32_t n_seqs, rows, n_rows;
+    const int32_t* d_seqs;
+    const int32_t* d_row_start;
+} fastcot_paged_rows;
+
+/* K and V of the rows into layer `layer`, at positions len + j (which need pages: rows without one are dropped).  d_k, d_v: device
+ * [n_rows][n_kv_heads][head_dim], rows row_stride elements apart (a multiple of 8; heads follow each other), aligned to 16 bytes, of act_dtype;
+ * fp32 values are rounded to nearest even for a bf16 cache; an fp32 cache takes fp32 only.  A sequence is named once. */
+int fastcot_paged_write(const fastcot_paged* cache, int32_t layer, const fastcot_paged_rows* rows, const void* d_k, const void* d_v,
+                        int64_t row_stride, int32_t act_dtype, void* hip_stream);
+
+/* Attention of the rows over layer `layer`: row at position p sees position k <= p (its own rows' K/V have been written) that has a
+ * page and, with window > 0, k > p - window or k < sinks (Eq. 2 conditioning as a mask; the window and the first tokens that stay
+ * visible are the caller's choice, window = 0: none).  Softmax of q . k / sqrt(head_dim).  d_q: device [n_rows][n_heads][head_dim], strides in elements (multiples of
+ * 8), aligned to 16 bytes, of act_dtype; d_out: [n_rows][n_heads * head_dim], out_row_stride elements apart (a multiple of 8), aligned to 16 bytes, of act_dtype;
+ * d_lse (nullable): fp32 [n_rows][n_heads], natural log of the sum of exp(score), for joining with attention over other keys.  n_heads: a multiple of
+ * n_kv_heads, at most 64 per K/V head.  act_dtype FASTCOT_BF16 needs a bf16 cache.  A row that sees nothing gets 0 (lse -infinity); nothing
+ * a row does not see reaches it, whatever is there.  Scores, softmax statistics and sums are fp32; with fp32 rows results are those of fp32 arithmetic.
+ * Rows that belong to no sequence are left as they are. */
+int fastcot_paged_attn(const fastcot_paged* cache, int32_t layer, const fastcot_paged_rows* rows, const void* d_q, int64_t q_row_stride,
+                       int64_t q_head_stride, int32_t n_heads, int32_t act_dtype, int32_t window, int32_t sinks, void* d_out,
+                       int64_t out_row_stride, float* d_lse, void* d_scratch, void* hip_stream);
+
 /* Measurement aids.  fastcot_stream_read: one plain streaming read of `bytes` (multiple of 16) device bytes at
  * d_src (16-byte aligned), shaped like the weight stream of the step's GEMMs (one workgroup per compute unit,
  * contiguous kilobytes per wave, 16 loads in flight); d_sink16 is a 16-byte device scratch the kernel may

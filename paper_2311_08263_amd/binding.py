@@ -15,7 +15,7 @@ import numpy as np
 from . import build as _build
 
 _lib = None
-vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+vp, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 N_KINDS = 16
 
 T = {"emb": 0, "wlm": 1, "gf": 2, "wq": 3, "wk": 4, "wv": 5, "wo": 6, "wg": 7, "wu": 8, "wd": 9, "g1": 10, "g2": 11}
@@ -43,6 +43,17 @@ class Config(ctypes.Structure):
     def from_shape(cls, s, max_batch: int, max_seq: int, window: int) -> "Config":
         return cls(s.n_layers, s.d_model, s.n_heads, s.n_kv_heads, s.head_dim, s.d_ffn, s.vocab, s.rms_eps,
                    s.rope_base, 0 if s.dtype == "f32" else 1, max_batch, max_seq, window)
+
+
+class PagedDesc(ctypes.Structure):
+    """fastcot_paged: a K/V cache in pages as the library sees it."""
+    _fields_ = [(n, i32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "max_seqs", "max_pages")] + \
+               [(n, vp) for n in ("k_pool", "v_pool", "table", "len", "ref")]
+
+
+class PagedRows(ctypes.Structure):
+    """fastcot_paged_rows: the rows of a pass."""
+    _fields_ = [("n_seqs", i32), ("rows", i32), ("n_rows", i32), ("d_seqs", vp), ("d_row_start", vp)]
 
 
 SYMBOLS = {
@@ -81,6 +92,17 @@ SYMBOLS = {
     "fastcot_canonical_bytes": (sz, [ctypes.POINTER(Config)]),
     "fastcot_canonical_offset": (sz, [ctypes.POINTER(Config), i32, i32]),
     "fastcot_pack_weights": (ctypes.c_int, [ctypes.POINTER(Config), vp, vp, vp]),
+    "fastcot_paged_pool_bytes": (sz, [ctypes.POINTER(PagedDesc)]),
+    "fastcot_paged_scratch_bytes": (sz, [ctypes.POINTER(PagedDesc)]),
+    "fastcot_paged_reset": (ctypes.c_int, [ctypes.POINTER(PagedDesc), vp]),
+    "fastcot_paged_grow": (ctypes.c_int, [ctypes.POINTER(PagedDesc), i32, vp, vp, vp, vp, vp]),
+    "fastcot_paged_advance": (ctypes.c_int, [ctypes.POINTER(PagedDesc), i32, vp, vp, vp, vp]),
+    "fastcot_paged_fork": (ctypes.c_int, [ctypes.POINTER(PagedDesc), i32, vp, vp, vp, vp, vp]),
+    "fastcot_paged_trim": (ctypes.c_int, [ctypes.POINTER(PagedDesc), i32, vp, i32, i32, vp, vp]),
+    "fastcot_paged_free": (ctypes.c_int, [ctypes.POINTER(PagedDesc), i32, vp, vp, vp]),
+    "fastcot_paged_compact": (ctypes.c_int, [ctypes.POINTER(PagedDesc), vp, vp, vp]),
+    "fastcot_paged_write": (ctypes.c_int, [ctypes.POINTER(PagedDesc), i32, ctypes.POINTER(PagedRows), vp, vp, i64, i32, vp]),
+    "fastcot_paged_attn": (ctypes.c_int, [ctypes.POINTER(PagedDesc), i32, ctypes.POINTER(PagedRows), vp, i64, i64, i32, i32, i32, i32, vp, i64, vp, vp, vp]),
 }
 
 
@@ -445,3 +467,157 @@ def lmhead_argmax(act, packed, V: int, want_logits: bool = False, scratch=None, 
                                        top2.data_ptr() if want_top2 else None,
                                        logits.data_ptr() if want_logits else None, scratch.data_ptr(), _stream_ptr()))
     return (ids, top, logits, top2) if want_top2 else (ids, top, logits)
+
+
+# ---------------------------------------------------------------------------- a K/V cache in pages
+def _bad(text: str):
+    return FastcotError(-1, text)
+
+
+class PagedCache:
+    """K and V of many sequences in pages (fastcot_paged in include/fastcot.h, which says what every call does).
+
+    k, v: pools [n_layers, n_pages, n_kv_heads, page_size // 32, 32 * head_dim] of dtype (torch.bfloat16 or torch.float32);
+    book: int32, the table, the lengths and the use counts one after the other.  What is not given is allocated; a book that is given is
+    taken as it is, otherwise every sequence starts empty.  Sequence numbers and counts are int32 tensors on the cache's device, statuses
+    come back as such (0, -1 EINVAL, -3 ECAPACITY).  Work is enqueued on torch's current stream of that device."""
+
+    def __init__(self, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype=None, n_layers: int = 1, max_seqs: int = 1,
+                 max_pages: Optional[int] = None, k=None, v=None, book=None, device=None):
+        torch = _torch()
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise _bad(f"a cache of {dtype}: torch.bfloat16 or torch.float32")
+        max_pages = n_pages if max_pages is None else max_pages
+        given = [t for t in (k, v, book) if t is not None]
+        dev = torch.device(device if device is not None else given[0].device if given else "cuda")
+        self.device = torch.device("cuda", torch.cuda.current_device() if dev.index is None else dev.index)
+        self.dtype = dtype
+        self._desc = PagedDesc(n_layers, n_pages, page_size, n_kv_heads, head_dim, 1 if dtype == torch.bfloat16 else 0, max_seqs, max_pages)
+        self._ref = ctypes.byref(self._desc)
+        L = lib()
+        nbytes, sbytes = L.fastcot_paged_pool_bytes(self._ref), L.fastcot_paged_scratch_bytes(self._ref)
+        if nbytes == 0:
+            raise _bad("invalid cache description")
+        shape = (n_layers, n_pages, n_kv_heads, page_size // 32, 32 * head_dim)
+        for t in (k, v):
+            if t is not None and (t.device != self.device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+                raise _bad(f"a pool is a contiguous {dtype} tensor {shape} on {self.device}")
+        words = max_seqs * max_pages + max_seqs + n_pages
+        if book is not None and (book.device != self.device or book.dtype != torch.int32 or tuple(book.shape) != (words,) or not book.is_contiguous()):
+            raise _bad(f"the book is a contiguous int32 tensor of {words} on {self.device}")
+        self.k = torch.empty(shape, dtype=dtype, device=self.device) if k is None else k
+        self.v = torch.empty(shape, dtype=dtype, device=self.device) if v is None else v
+        self.book = torch.empty(words, dtype=torch.int32, device=self.device) if book is None else book
+        self.table = self.book[:max_seqs * max_pages].view(max_seqs, max_pages)
+        self.len = self.book[max_seqs * max_pages:max_seqs * (max_pages + 1)]
+        self.ref = self.book[max_seqs * (max_pages + 1):]
+        self.scratch = torch.zeros(sbytes, dtype=torch.uint8, device=self.device)
+        d = self._desc
+        d.k_pool, d.v_pool = self.k.data_ptr(), self.v.data_ptr()
+        d.table, d.len, d.ref = self.table.data_ptr(), self.len.data_ptr(), self.ref.data_ptr()
+        if book is None:
+            self._call(L.fastcot_paged_reset, self._ref)
+        torch.cuda.synchronize(self.device)          # whatever stream the calls run on, they find it made
+
+    def _call(self, fn, *args) -> None:
+        torch, dev = _gpu_torch, self.device.index
+        if torch.cuda.current_device() == dev:
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+        else:
+            with torch.cuda.device(dev):
+                rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+        _check(rc)
+
+    def _ints(self, t, what: str, n: Optional[int] = None):
+        if t.dtype != _gpu_torch.int32 or t.device != self.device or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+            raise _bad(f"{what}: a contiguous int32 tensor{'' if n is None else f' of {n}'} on {self.device}")
+        return t.data_ptr()
+
+    def _entries(self, fn, a, b, *more):
+        status = _gpu_torch.empty(a.numel(), dtype=_gpu_torch.int32, device=self.device)
+        args = (self._ints(a, "sequences"),) + (() if b is None else (self._ints(b, "the second argument", a.numel()),))
+        self._call(fn, self._ref, a.numel(), *args, *more[:-1], status.data_ptr(), *more[-1])
+        return status
+
+    def grow(self, seqs, rows):
+        """Pages for the next rows[i] positions of each sequence."""
+        return self._entries(lib().fastcot_paged_grow, seqs, rows, (self.scratch.data_ptr(),))
+
+    def advance(self, seqs, rows):
+        """len += rows[i]: the rows are committed."""
+        return self._entries(lib().fastcot_paged_advance, seqs, rows, ())
+
+    def fork(self, src, dst):
+        """The empty sequence dst[i] continues src[i]."""
+        return self._entries(lib().fastcot_paged_fork, src, dst, (self.scratch.data_ptr(),))
+
+    def trim(self, seqs, window: int, sinks: int = 0):
+        """Pages that a sliding window has left behind leave the sequences."""
+        return self._entries(lib().fastcot_paged_trim, seqs, None, window, sinks, ())
+
+    def free(self, seqs):
+        """The sequences end."""
+        return self._entries(lib().fastcot_paged_free, seqs, None, ())
+
+    def compact(self):
+        """Pages in use move to the front of the pools; returns their number (a device int32)."""
+        used = _gpu_torch.empty((), dtype=_gpu_torch.int32, device=self.device)
+        self._call(lib().fastcot_paged_compact, self._ref, used.data_ptr(), self.scratch.data_ptr())
+        return used
+
+    def _rows(self, n_rows: int, seqs, row_start, max_rows: Optional[int]) -> PagedRows:
+        n_seqs = seqs.numel() if seqs is not None else row_start.numel() - 1 if row_start is not None else self._desc.max_seqs
+        ps = self._ints(seqs, "sequences") if seqs is not None else None
+        if row_start is None:
+            if n_rows % max(n_seqs, 1) or (n_rows and not n_seqs):
+                raise _bad(f"{n_rows} rows of {n_seqs} sequences: give row_start")
+            return PagedRows(n_seqs, n_rows // max(n_seqs, 1), n_rows, ps, None)
+        return PagedRows(n_seqs, n_rows if max_rows is None else max_rows, n_rows, ps, self._ints(row_start, "row_start", n_seqs + 1))
+
+    def _act(self, t, shape, what: str) -> int:
+        torch = _gpu_torch
+        if t.device != self.device or tuple(t.shape[1:]) != shape or t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16) or \
+                (t.stride(2) != 1 and t.numel()):
+            raise _bad(f"{what}: fp32 or bf16 rows x {shape} on {self.device}, head elements next to each other")
+        return 0 if t.dtype == torch.float32 else 1
+
+    def write(self, k, v, layer: int = 0, seqs=None, row_start=None, max_rows: Optional[int] = None) -> None:
+        """k, v [rows, n_kv_heads, head_dim] of the sequences' next positions into a layer.  Without row_start every sequence has as many rows;
+        with it (int32 on the device, one more entry than sequences) sequence i has rows row_start[i] .. row_start[i + 1] - 1, at most max_rows."""
+        d = self._desc
+        shape = (d.n_kv_heads, d.head_dim)
+        act = self._act(k, shape, "k")
+        if self._act(v, shape, "v") != act or v.shape != k.shape:
+            raise _bad("k and v differ in type or rows")
+        n, row = k.shape[0], d.n_kv_heads * d.head_dim
+        if d.n_kv_heads > 1 and n and (k.stride(1) != d.head_dim or v.stride(1) != d.head_dim):
+            raise _bad("the heads of a row of k and v follow each other")
+        if n > 1:
+            row = k.stride(0)
+            if v.stride(0) != row:
+                raise _bad("the rows of k and v are at different strides")
+        r = self._rows(n, seqs, row_start, max_rows)
+        self._call(lib().fastcot_paged_write, self._ref, layer, ctypes.byref(r), k.data_ptr(), v.data_ptr(), row, act)
+
+    def attn(self, q, layer: int = 0, seqs=None, row_start=None, max_rows: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
+             want_lse: bool = False, scratch=None):
+        """q [rows, heads, head_dim] (rows as for write, already written) -> out [rows, heads * head_dim] of q's type, and with want_lse the log of
+        the sum of exp(score), fp32 [rows, heads].  Calls that may overlap in time need a scratch of their own (zeros like self.scratch)."""
+        torch, d = _gpu_torch, self._desc
+        n, H = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+        act = self._act(q, (H, d.head_dim), "q")
+        if out is None:
+            out = torch.empty(n, H * d.head_dim, dtype=q.dtype, device=self.device)
+        elif out.dtype != q.dtype or out.device != self.device or tuple(out.shape) != (n, H * d.head_dim) or (out.stride(1) != 1 and n):
+            raise _bad(f"out: {q.dtype} {(n, H * d.head_dim)} on {self.device}")
+        lse = torch.empty(n, H, dtype=torch.float32, device=self.device) if want_lse else None
+        if scratch is None:
+            scratch = self.scratch
+        elif scratch.device != self.device or not scratch.is_contiguous() or scratch.numel() * scratch.element_size() < self.scratch.numel():
+            raise _bad(f"scratch: {self.scratch.numel()} zeroed bytes on {self.device}")
+        r = self._rows(n, seqs, row_start, max_rows)
+        self._call(lib().fastcot_paged_attn, self._ref, layer, ctypes.byref(r), q.data_ptr(), q.stride(0) if n > 1 else H * d.head_dim,
+                   q.stride(1) if H > 1 else d.head_dim, H, act, window, sinks, out.data_ptr(), out.stride(0) if n > 1 else H * d.head_dim,
+                   lse.data_ptr() if want_lse else None, scratch.data_ptr())
+        return (out, lse) if want_lse else out

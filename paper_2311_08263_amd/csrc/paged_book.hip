@@ -1,0 +1,507 @@
+// The K/V cache in pages: tables and use counts, copies of pages, K/V of new rows, and the C entry points.
+//
+// The bookkeeping of a call is one workgroup of sixteen waves: sixteen lanes look at an entry's part of the table, the entries' needs are
+// summed in order, and the use counts are walked 4096 pages at a time until enough free ones are found, so that pages go out lowest
+// first whatever the timing.  It is bound by its chain of dependent loads (entry, length, table, use counts), about a microsecond each.
+// Page data move in blocks of 32 positions of one head (8 KB at 128 bf16 elements), a workgroup each: bound by HBM, bytes read and written once.
+#include <limits.h>
+#include <stdio.h>
+#include "paged.h"
+#include "gemmco.h"      // fc_num_cus
+
+#define PG_WG 1024
+#define PG_HEAD 8192         // bytes of the scratch in front of the lists: [0] number of moves
+#define NONE_FIRST INT_MAX
+
+// exclusive prefix sum over the workgroup; *total: the sum.  lds: 17 ints
+__device__ inline int pg_scan(int v, int* lds, int* total) {
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { const int y = __shfl_up(x, d, 64); if (lane >= d) x += y; }
+    __syncthreads();                              // (lds may still be read from the last call)
+    if (lane == 63) lds[wv] = x;
+    __syncthreads();
+    if (wv == 0) {
+        int t = lane < PG_WG / 64 ? lds[lane] : 0, y = t;
+#pragma unroll
+        for (int d = 1; d < PG_WG / 64; d <<= 1) { const int z = __shfl_up(y, d, 64); if (lane >= d) y += z; }
+        if (lane < PG_WG / 64) lds[lane] = y - t;
+        if (lane == PG_WG / 64 - 1) lds[16] = y;
+    }
+    __syncthreads();
+    *total = lds[16];
+    return lds[wv] + x - v;
+}
+// the lowest free pages, up to `want` of them, into list; how many there are (at most `want`).  For the whole workgroup
+__device__ inline int pg_find_free(const PagedView& c, int want, int* list, int* lds) {
+    int found = 0;
+    for (int base = 0; base < c.N && found < want; base += 4 * PG_WG) {
+        const int p0 = base + 4 * (int)threadIdx.x;
+        int f[4], n = 0, total;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { f[e] = p0 + e < c.N && c.ref[p0 + e] == 0; n += f[e]; }
+        int at = found + pg_scan(n, lds, &total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (f[e]) { if (at < want) list[at] = p0 + e; ++at; }
+        found += total;
+    }
+    __syncthreads();
+    return found < want ? found : want;
+}
+// index of the first entry of the call that names each sequence
+__device__ inline void pg_first(const PagedView& c, int count, const int32_t* seqs, int* first) {
+    for (int s = threadIdx.x; s < c.S; s += PG_WG) first[s] = NONE_FIRST;
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += PG_WG) { const int s = seqs[i]; if (s >= 0 && s < c.S) atomicMin(&first[s], i); }
+    __syncthreads();
+}
+__device__ inline bool pg_none(const PagedView& c, int page) { return page < 0 || page >= c.N; }
+// number of set lanes among the sixteen of this one's group, and among those in front of it
+__device__ inline int pg_group_count(bool x, int* before) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t m = (uint32_t)(__ballot(x) >> (lane & 48)) & 0xFFFFu;
+    *before = __popc(m & ((1u << (lane & 15)) - 1));
+    return __popc(m);
+}
+// needs of the entries (below zero: a status) -> exclusive sums in pre; the sum of all.  For the whole workgroup
+__device__ inline int pg_sum_needs(int count, const int* need, int* pre, int* lds) {
+    int sum = 0;
+    for (int base = 0; base < count; base += PG_WG) {
+        const int i = base + threadIdx.x;
+        int total;
+        const int v = i < count && need[i] > 0 ? need[i] : 0, at = pg_scan(v, lds, &total);
+        if (i < count) pre[i] = sum + at;
+        sum += total;
+    }
+    __syncthreads();
+    return sum;
+}
+
+// slots [n / P, end) of a sequence that the positions n .. n + rows - 1 fall into; end > MP: they pass the table
+__device__ inline int64_t pg_end_slot(const PagedView& c, int n, int rows) {
+    const int64_t P = (int64_t)32 << c.pb;
+    return (n + (int64_t)rows + P - 1) >> (c.pb + 5);
+}
+
+__global__ __launch_bounds__(PG_WG) void k_paged_grow(PagedView c, int count, const int32_t* seqs, const int32_t* rows, int32_t* status, int* list) {
+    __shared__ int first[PG_MAX_SEQS], need[PG_MAX_SEQS], pre[PG_MAX_SEQS], lds[17];
+    const int grp = threadIdx.x >> 4, l = threadIdx.x & 15;
+    pg_first(c, count, seqs, first);
+    for (int i = grp; i < count; i += PG_WG / 16) {
+        const int s = seqs[i], r = rows[i];
+        int v = FASTCOT_EINVAL, before;
+        if (s >= 0 && s < c.S && r >= 0 && first[s] == i) {
+            const int n = pg_len(c, s);
+            const int64_t end = pg_end_slot(c, n, r);
+            v = FASTCOT_ECAPACITY;
+            if (end <= c.MP) {
+                v = 0;
+                for (int k = n >> (c.pb + 5); k < end; k += 16) v += pg_group_count(k + l < end && pg_none(c, c.table[(size_t)s * c.MP + k + l]), &before);
+            }
+        }
+        if (l == 0) need[i] = v;
+    }
+    __syncthreads();
+    const int total = pg_sum_needs(count, need, pre, lds), found = pg_find_free(c, total, list, lds);
+    for (int i = grp; i < count; i += PG_WG / 16) {
+        const int v = need[i];
+        const bool given = v >= 0 && (v == 0 || pre[i] + v <= found);
+        if (l == 0 && status) status[i] = v < 0 ? v : given ? 0 : FASTCOT_ECAPACITY;
+        if (v <= 0 || !given) continue;
+        const int s = seqs[i], n = pg_len(c, s);
+        const int end = (int)pg_end_slot(c, n, rows[i]);
+        int at = pre[i], before;
+        for (int k = n >> (c.pb + 5); k < end; k += 16) {
+            const bool want = k + l < end && pg_none(c, c.table[(size_t)s * c.MP + k + l]);
+            const int m = pg_group_count(want, &before);
+            if (want) {
+                const int page = list[at + before];
+                c.table[(size_t)s * c.MP + k + l] = page;
+                c.ref[page] = 1;
+            }
+            at += m;
+        }
+    }
+}
+
+__global__ __launch_bounds__(PG_WG) void k_paged_advance(PagedView c, int count, const int32_t* seqs, const int32_t* rows, int32_t* status) {
+    __shared__ int first[PG_MAX_SEQS];
+    const int grp = threadIdx.x >> 4, l = threadIdx.x & 15;
+    pg_first(c, count, seqs, first);
+    for (int i = grp; i < count; i += PG_WG / 16) {
+        const int s = seqs[i], r = rows[i];
+        int v = FASTCOT_EINVAL, before, n = 0;
+        if (s >= 0 && s < c.S && r >= 0 && first[s] == i) {
+            n = pg_len(c, s);
+            const int64_t end = pg_end_slot(c, n, r);
+            v = FASTCOT_ECAPACITY;
+            if (end <= c.MP) {
+                int missing = 0;
+                for (int k = n >> (c.pb + 5); k < end; k += 16) missing += pg_group_count(k + l < end && pg_none(c, c.table[(size_t)s * c.MP + k + l]), &before);
+                if (!missing) v = 0;
+            }
+        }
+        if (l == 0) {
+            if (v == 0) c.len[s] = n + r;
+            if (status) status[i] = v;
+        }
+    }
+}
+
+// moves: list of page copies (from, to, blocks of 32 positions), their number in *n_moves
+__global__ __launch_bounds__(PG_WG) void k_paged_fork(PagedView c, int count, const int32_t* src, const int32_t* dst, int32_t* status, int* n_moves, int* from,
+                                                      int* to, int* blocks) {
+    __shared__ int first[PG_MAX_SEQS], need[PG_MAX_SEQS], pre[PG_MAX_SEQS], lds[17];
+    const int grp = threadIdx.x >> 4, l = threadIdx.x & 15, P = 32 << c.pb;
+    pg_first(c, count, dst, first);
+    for (int i = threadIdx.x; i < count; i += PG_WG) {
+        const int s = src[i], d = dst[i];
+        int v = FASTCOT_EINVAL;
+        if (s >= 0 && s < c.S && d >= 0 && d < c.S && first[d] == i && first[s] == NONE_FIRST && c.len[d] == 0 && pg_none(c, c.table[(size_t)d * c.MP])) {
+            const int n = pg_len(c, s);
+            v = n & (P - 1) && !pg_none(c, c.table[(size_t)s * c.MP + (n >> (c.pb + 5))]);
+        }
+        need[i] = v;
+    }
+    __syncthreads();
+    const int total = pg_sum_needs(count, need, pre, lds), found = pg_find_free(c, total, to, lds);
+    for (int i = grp; i < count; i += PG_WG / 16) {
+        const int v = need[i];
+        const bool given = v >= 0 && (v == 0 || pre[i] < found);
+        if (l == 0 && status) status[i] = v < 0 ? v : given ? 0 : FASTCOT_ECAPACITY;
+        if (!given) continue;
+        const int s = src[i], d = dst[i], n = pg_len(c, s), last = n >> (c.pb + 5);
+        for (int k = l; k < last; k += 16) {
+            const int page = c.table[(size_t)s * c.MP + k];
+            c.table[(size_t)d * c.MP + k] = page;
+            if (!pg_none(c, page)) atomicAdd(&c.ref[page], 1);
+        }
+        if (l == 0) {
+            c.len[d] = n;
+            if (v) {
+                const int at = pre[i], page = to[at];
+                c.table[(size_t)d * c.MP + last] = page;
+                c.ref[page] = 1;
+                from[at] = c.table[(size_t)s * c.MP + last];
+                blocks[at] = ((n & (P - 1)) + 31) >> 5;
+            }
+        }
+    }
+    if (threadIdx.x == 0) *n_moves = found;
+}
+
+// a workgroup per entry; sinks < 0: every page leaves.  An entry exchanges what it takes out of the table, so one that is named twice leaves once
+__global__ __launch_bounds__(256) void k_paged_leave(PagedView c, const int32_t* seqs, int window, int sinks, int32_t* status) {
+    const int i = blockIdx.x, s = seqs[i];
+    const bool ok = s >= 0 && s < c.S;
+    if (threadIdx.x == 0 && status) status[i] = ok ? 0 : FASTCOT_EINVAL;
+    if (!ok) return;
+    const int P = 32 << c.pb, n = c.len[s];
+    int k0 = 0, k1 = c.MP;
+    if (sinks >= 0) {
+        // pages k with k * P >= sinks and (k + 1) * P - 1 <= n - window
+        k0 = (int)(((int64_t)sinks + P - 1) >> (c.pb + 5));
+        const int64_t seen = (int64_t)n - window + 1;
+        k1 = seen <= 0 ? 0 : (int)(seen >> (c.pb + 5));
+        if (k1 > c.MP) k1 = c.MP;
+    }
+    for (int k = k0 + threadIdx.x; k < k1; k += 256) {
+        const int page = atomicExch(&c.table[(size_t)s * c.MP + k], -1);
+        if (!pg_none(c, page)) atomicSub(&c.ref[page], 1);
+    }
+    if (sinks < 0) {
+        __syncthreads();
+        if (threadIdx.x == 0) c.len[s] = 0;
+    }
+}
+
+__global__ __launch_bounds__(PG_WG) void k_paged_compact(PagedView c, int32_t* d_used, int* n_moves, int* from, int* to, int* map) {
+    __shared__ int lds[17];
+    int used = 0, moves = 0, holes = 0, total;
+    for (int base = 0; base < c.N; base += 4 * PG_WG) {
+        const int p0 = base + 4 * (int)threadIdx.x;
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) n += p0 + e < c.N && c.ref[p0 + e] > 0;
+        pg_scan(n, lds, &total);
+        used += total;
+    }
+    for (int base = 0; base < c.N; base += 4 * PG_WG) {
+        const int p0 = base + 4 * (int)threadIdx.x;
+        int in[4], n = 0;                                // pages that move in the upper half of a word, free places in the lower one
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int p = p0 + e;
+            in[e] = p >= c.N ? 0 : c.ref[p] > 0 ? (p >= used ? 1 << 16 : 0) : p < used ? 1 : 0;
+            if (p < c.N) map[p] = p;
+            n += in[e];
+        }
+        const int at = pg_scan(n, lds, &total);
+        int a = moves + (at >> 16), b = holes + (at & 0xFFFF);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (in[e] == 1) to[b++] = p0 + e;
+            else if (in[e]) from[a++] = p0 + e;
+        }
+        moves += total >> 16;
+        holes += total & 0xFFFF;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < moves; i += PG_WG) {   // (as many free places among the first `used` as pages in use behind them)
+        c.ref[to[i]] = c.ref[from[i]];
+        c.ref[from[i]] = 0;
+        map[from[i]] = to[i];
+    }
+    if (threadIdx.x == 0) { *n_moves = moves; if (d_used) *d_used = used; }
+}
+
+// Copies page data by a list of moves, block by block; blocks == NULL: whole pages.  With a map the table follows.
+__global__ __launch_bounds__(256) void k_paged_move(PagedView c, int block16, const int* n_moves, const int* from, const int* to, const int* blocks, const int* map) {
+    const int moves = *n_moves, tid = threadIdx.x;
+    if (map)
+        for (size_t i = (size_t)blockIdx.x * 256 + tid; i < (size_t)c.S * c.MP; i += (size_t)gridDim.x * 256) {
+            const int page = c.table[i];
+            if (!pg_none(c, page)) c.table[i] = map[page];
+        }
+    const int PB = 1 << c.pb;
+    const int64_t per = (int64_t)c.L * 2 * c.Hkv << c.pb, all = per * moves;
+    for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
+        const int m = (int)(x / per);
+        const uint32_t y = (uint32_t)(x - m * per), blk = y & (PB - 1), z = y >> c.pb, h = z % c.Hkv, w = z / c.Hkv;
+        if (blocks && (int)blk >= blocks[m]) continue;
+        char* pool = w & 1 ? c.v : c.k;
+        const size_t layer = (size_t)(w >> 1) * c.N;
+        const uint4* a = (const uint4*)pool + ((((layer + from[m]) * c.Hkv + h) << c.pb) + blk) * block16;
+        uint4* b = (uint4*)pool + ((((layer + to[m]) * c.Hkv + h) << c.pb) + blk) * block16;
+        for (int e = tid; e < block16; e += 256) b[e] = a[e];
+    }
+}
+
+__global__ __launch_bounds__(256) void k_paged_reset(PagedView c) {
+    const size_t i0 = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)gridDim.x * 256;
+    for (size_t i = i0; i < (size_t)c.S * c.MP; i += step) c.table[i] = -1;
+    for (size_t i = i0; i < (size_t)c.S; i += step) c.len[i] = 0;
+    for (size_t i = i0; i < (size_t)c.N; i += step) c.ref[i] = 0;
+}
+
+// eight values of a row in the cache's type
+__device__ inline void pg_load8(const void* p, size_t at, int act, float* v) {
+    if (act == FASTCOT_BF16) {
+        const uint4 u = *(const uint4*)((const bf16_t*)p + at);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(w[e] << 16); v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
+    } else {
+        const float4 x = *(const float4*)((const float*)p + at), y = *(const float4*)((const float*)p + at + 4);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    }
+}
+
+// grid: x over a sequence's rows x heads x eights of a head, y over sequences
+template <int DT>
+__global__ __launch_bounds__(256) void k_paged_write(PagedView c, PagedRows r, int Dh, char* kl, char* vl, const void* k, const void* v, int64_t row_stride, int act) {
+    typedef typename std::conditional<DT == FASTCOT_BF16, bf16_t, float>::type T;
+    const int i = blockIdx.y, D8 = Dh >> 3, s = pg_seq(r, c, i);
+    int first, count;
+    pg_rows(r, i, first, count);
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int d8 = (int)(x % D8), h = (int)(x / D8 % c.Hkv), j = (int)(x / D8 / c.Hkv);
+    if (s < 0 || j >= count) return;
+    const int64_t pos = (int64_t)pg_len(c, s) + j;
+    const int64_t slot = pos >> (c.pb + 5);
+    if (slot >= c.MP) return;
+    const int page = c.table[(size_t)s * c.MP + slot];
+    if (pg_none(c, page)) return;
+    float a[8], b[8];
+    const size_t at = (size_t)(first + j) * row_stride + (size_t)h * Dh + 8 * d8;
+    pg_load8(k, at, act, a);
+    pg_load8(v, at, act, b);
+    const int p = (int)(pos & ((32 << c.pb) - 1));
+    const size_t base = (((size_t)page * c.Hkv + h) << c.pb) * 32 * Dh;
+    T* kd = (T*)kl + base; T* vd = (T*)vl + base;
+    if constexpr (DT == FASTCOT_BF16) {
+        *(uint4*)(kd + k_index(p, 8 * d8, Dh)) = make_uint4(pk_bf16(a[0], a[1]), pk_bf16(a[2], a[3]), pk_bf16(a[4], a[5]), pk_bf16(a[6], a[7]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vd[v_index(8 * d8 + e, p, Dh)] = (bf16_t)(pk_bf16(b[e], 0.f) & 0xFFFF);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { kd[k_index(p, 8 * d8 + e, Dh)] = a[e]; vd[v_index(8 * d8 + e, p, Dh)] = b[e]; }
+    }
+}
+
+// ------------------------------------------------------------------ C entry points
+#define FAIL(rc, ...) do { char text_[256]; snprintf(text_, sizeof text_, __VA_ARGS__); fc_set_error(text_); return rc; } while (0)
+
+static bool head_dim_ok(int Dh) { return Dh == 32 || Dh == 64 || Dh == 96 || Dh == 128 || Dh == 192 || Dh == 256; }
+static bool shape_ok(const fastcot_paged* c) {
+    return c && c->n_layers >= 1 && c->n_layers <= 4096 && c->n_pages >= 1 && c->n_pages <= PG_MAX_PAGES && c->page_size >= 32 && c->page_size <= 4096 &&
+           !(c->page_size & (c->page_size - 1)) && c->n_kv_heads >= 1 && c->n_kv_heads <= 4096 && head_dim_ok(c->head_dim) &&
+           (c->dtype == FASTCOT_F32 || c->dtype == FASTCOT_BF16) && c->max_seqs >= 1 && c->max_seqs <= PG_MAX_SEQS && c->max_pages >= 1 &&
+           (int64_t)c->max_pages * c->page_size <= (int64_t)1 << 30;
+}
+static size_t esz_of(const fastcot_paged* c) { return c->dtype == FASTCOT_BF16 ? 2 : 4; }
+static size_t page_bytes(const fastcot_paged* c) { return (size_t)c->n_kv_heads * c->page_size * c->head_dim * esz_of(c); }
+static size_t list_bytes(const fastcot_paged* c) { return FC_ALIGN((size_t)c->n_pages * 4); }
+
+static int view_of(const char* name, const fastcot_paged* c, PagedView* v) {
+    if (!shape_ok(c)) FAIL(FASTCOT_EINVAL, "%s: bad cache description", name);
+    if (!c->k_pool || !c->v_pool || !c->table || !c->len || !c->ref) FAIL(FASTCOT_EINVAL, "%s: NULL device pointer in the cache", name);
+    if (((uintptr_t)c->k_pool | (uintptr_t)c->v_pool) & 15) FAIL(FASTCOT_EINVAL, "%s: pools have to be aligned to 16 bytes", name);
+    if (((uintptr_t)c->table | (uintptr_t)c->len | (uintptr_t)c->ref) & 3) FAIL(FASTCOT_EINVAL, "%s: misaligned int32 array", name);
+    v->L = c->n_layers; v->N = c->n_pages; v->Hkv = c->n_kv_heads; v->Dh = c->head_dim; v->S = c->max_seqs; v->MP = c->max_pages;
+    v->pb = __builtin_ctz((unsigned)c->page_size) - 5;
+    v->k = (char*)c->k_pool; v->v = (char*)c->v_pool; v->table = c->table; v->len = c->len; v->ref = c->ref;
+    return 0;
+}
+static int entries_of(const char* name, const fastcot_paged* c, int32_t count, const void* a, const void* b) {
+    if (count < 0 || count > c->max_seqs) FAIL(FASTCOT_EINVAL, "%s: count %d outside 0..max_seqs", name, (int)count);
+    if (count && (!a || !b)) FAIL(FASTCOT_EINVAL, "%s: NULL device pointer", name);
+    return 0;
+}
+static int scratch_of(const char* name, void* d_scratch) {
+    if (!d_scratch || ((uintptr_t)d_scratch & 255)) FAIL(FASTCOT_EINVAL, "%s: scratch has to be given, aligned to 256 bytes", name);
+    return 0;
+}
+static int rows_of(const char* name, const fastcot_paged_rows* r, int32_t layer, int32_t act, const fastcot_paged* c, PagedRows* o) {
+    if (!r || r->n_seqs < 0 || r->rows < 0 || r->n_rows < 0) FAIL(FASTCOT_EINVAL, "%s: bad rows", name);
+    if (r->n_seqs > 65535) FAIL(FASTCOT_EINVAL, "%s: more than 65535 sequences", name);
+    if (!r->d_seqs && r->n_seqs > c->max_seqs) FAIL(FASTCOT_EINVAL, "%s: more sequences than the cache has", name);
+    if (!r->d_row_start && (int64_t)r->n_seqs * r->rows != r->n_rows) FAIL(FASTCOT_EINVAL, "%s: n_rows is not n_seqs * rows", name);
+    if (layer < 0 || layer >= c->n_layers) FAIL(FASTCOT_EINVAL, "%s: layer %d outside the cache", name, (int)layer);
+    if (act != FASTCOT_F32 && act != FASTCOT_BF16) FAIL(FASTCOT_EINVAL, "%s: unknown type of rows", name);
+    if (act == FASTCOT_BF16 && c->dtype == FASTCOT_F32) FAIL(FASTCOT_EINVAL, "%s: an fp32 cache takes fp32 rows", name);
+    o->B = r->n_seqs; o->R = r->rows < r->n_rows ? r->rows : r->n_rows; o->n_rows = r->n_rows; o->seqs = r->d_seqs; o->start = r->d_row_start;
+    return 0;
+}
+static int launched(const char* name, hipError_t e) {
+    if (e != hipSuccess) FAIL(FASTCOT_EHIP, "%s: launch failed (%s)", name, hipGetErrorString(e));
+    return 0;
+}
+#define TRY(x) do { const int rc_ = (x); if (rc_) return rc_; } while (0)
+
+extern "C" size_t fastcot_paged_pool_bytes(const fastcot_paged* c) {
+    return shape_ok(c) ? (size_t)c->n_layers * c->n_pages * page_bytes(c) : 0;
+}
+extern "C" size_t fastcot_paged_scratch_bytes(const fastcot_paged* c) {
+    return shape_ok(c) ? PG_HEAD + 3 * list_bytes(c) + fc_paged_attn_scratch_bytes(c->head_dim) : 0;
+}
+extern "C" int fastcot_paged_reset(const fastcot_paged* c, void* hip_stream) {
+    const char* name = "fastcot_paged_reset";
+    PagedView v;
+    TRY(view_of(name, c, &v));
+    k_paged_reset<<<256, 256, 0, (hipStream_t)hip_stream>>>(v);
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_grow(const fastcot_paged* c, int32_t count, const int32_t* d_seqs, const int32_t* d_rows, int32_t* d_status, void* d_scratch,
+                                  void* hip_stream) {
+    const char* name = "fastcot_paged_grow";
+    PagedView v;
+    TRY(view_of(name, c, &v));
+    TRY(entries_of(name, c, count, d_seqs, d_rows));
+    TRY(scratch_of(name, d_scratch));
+    if (!count) return 0;
+    k_paged_grow<<<1, PG_WG, 0, (hipStream_t)hip_stream>>>(v, count, d_seqs, d_rows, d_status, (int*)((char*)d_scratch + PG_HEAD));
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_advance(const fastcot_paged* c, int32_t count, const int32_t* d_seqs, const int32_t* d_rows, int32_t* d_status, void* hip_stream) {
+    const char* name = "fastcot_paged_advance";
+    PagedView v;
+    TRY(view_of(name, c, &v));
+    TRY(entries_of(name, c, count, d_seqs, d_rows));
+    if (!count) return 0;
+    k_paged_advance<<<1, PG_WG, 0, (hipStream_t)hip_stream>>>(v, count, d_seqs, d_rows, d_status);
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_fork(const fastcot_paged* c, int32_t count, const int32_t* d_src, const int32_t* d_dst, int32_t* d_status, void* d_scratch,
+                                  void* hip_stream) {
+    const char* name = "fastcot_paged_fork";
+    PagedView v;
+    TRY(view_of(name, c, &v));
+    TRY(entries_of(name, c, count, d_src, d_dst));
+    TRY(scratch_of(name, d_scratch));
+    if (!count) return 0;
+    char* l = (char*)d_scratch + PG_HEAD;
+    int *n = (int*)d_scratch, *from = (int*)l, *to = (int*)(l + list_bytes(c)), *blocks = (int*)(l + 2 * list_bytes(c));
+    hipStream_t st = (hipStream_t)hip_stream;
+    k_paged_fork<<<1, PG_WG, 0, st>>>(v, count, d_src, d_dst, d_status, n, from, to, blocks);
+    TRY(launched(name, hipGetLastError()));
+    k_paged_move<<<8 * fc_num_cus(), 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, blocks, nullptr);
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_trim(const fastcot_paged* c, int32_t count, const int32_t* d_seqs, int32_t window, int32_t sinks, int32_t* d_status, void* hip_stream) {
+    const char* name = "fastcot_paged_trim";
+    PagedView v;
+    TRY(view_of(name, c, &v));
+    TRY(entries_of(name, c, count, d_seqs, d_seqs));
+    if (window < 1 || sinks < 0) FAIL(FASTCOT_EINVAL, "%s: window below 1 or sinks below 0", name);
+    if (!count) return 0;
+    k_paged_leave<<<count, 256, 0, (hipStream_t)hip_stream>>>(v, d_seqs, window, sinks, d_status);
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_free(const fastcot_paged* c, int32_t count, const int32_t* d_seqs, int32_t* d_status, void* hip_stream) {
+    const char* name = "fastcot_paged_free";
+    PagedView v;
+    TRY(view_of(name, c, &v));
+    TRY(entries_of(name, c, count, d_seqs, d_seqs));
+    if (!count) return 0;
+    k_paged_leave<<<count, 256, 0, (hipStream_t)hip_stream>>>(v, d_seqs, 0, -1, d_status);
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_compact(const fastcot_paged* c, int32_t* d_used, void* d_scratch, void* hip_stream) {
+    const char* name = "fastcot_paged_compact";
+    PagedView v;
+    TRY(view_of(name, c, &v));
+    TRY(scratch_of(name, d_scratch));
+    char* l = (char*)d_scratch + PG_HEAD;
+    int *n = (int*)d_scratch, *from = (int*)l, *to = (int*)(l + list_bytes(c)), *map = (int*)(l + 2 * list_bytes(c));
+    hipStream_t st = (hipStream_t)hip_stream;
+    k_paged_compact<<<1, PG_WG, 0, st>>>(v, d_used, n, from, to, map);
+    TRY(launched(name, hipGetLastError()));
+    k_paged_move<<<8 * fc_num_cus(), 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, nullptr, map);
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_write(const fastcot_paged* c, int32_t layer, const fastcot_paged_rows* rows, const void* d_k, const void* d_v, int64_t row_stride,
+                                   int32_t act_dtype, void* hip_stream) {
+    const char* name = "fastcot_paged_write";
+    PagedView v;
+    PagedRows r;
+    TRY(view_of(name, c, &v));
+    TRY(rows_of(name, rows, layer, act_dtype, c, &r));
+    if (!r.B || !r.R || !r.n_rows) return 0;
+    if (!d_k || !d_v || (((uintptr_t)d_k | (uintptr_t)d_v) & 15)) FAIL(FASTCOT_EINVAL, "%s: K and V have to be given, aligned to 16 bytes", name);
+    if (row_stride % 8 || row_stride < (int64_t)c->n_kv_heads * c->head_dim) FAIL(FASTCOT_EINVAL, "%s: row stride below a row or no multiple of 8", name);
+    char* kl = v.k + (size_t)layer * c->n_pages * page_bytes(c);
+    char* vl = v.v + (size_t)layer * c->n_pages * page_bytes(c);
+    const int64_t per = (int64_t)r.R * c->n_kv_heads * (c->head_dim / 8), gx = (per + 255) / 256;
+    if (gx > 0x7FFFFFFF) FAIL(FASTCOT_ECAPACITY, "%s: too many rows of one sequence", name);
+    const dim3 grid((unsigned)gx, (unsigned)r.B);
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (c->dtype == FASTCOT_BF16) k_paged_write<FASTCOT_BF16><<<grid, 256, 0, st>>>(v, r, c->head_dim, kl, vl, d_k, d_v, row_stride, act_dtype);
+    else k_paged_write<FASTCOT_F32><<<grid, 256, 0, st>>>(v, r, c->head_dim, kl, vl, d_k, d_v, row_stride, act_dtype);
+    return launched(name, hipGetLastError());
+}
+extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const fastcot_paged_rows* rows, const void* d_q, int64_t q_row_stride,
+                                  int64_t q_head_stride, int32_t n_heads, int32_t act_dtype, int32_t window, int32_t sinks, void* d_out, int64_t out_row_stride,
+                                  float* d_lse, void* d_scratch, void* hip_stream) {
+    const char* name = "fastcot_paged_attn";
+    PagedAttnArgs a;
+    TRY(view_of(name, c, &a.c));
+    TRY(rows_of(name, rows, layer, act_dtype, c, &a.r));
+    TRY(scratch_of(name, d_scratch));
+    if (n_heads < 1 || n_heads % c->n_kv_heads || n_heads / c->n_kv_heads > 64) FAIL(FASTCOT_EINVAL, "%s: heads are no multiple (up to 64) of the cache's", name);
+    if (window < 0 || sinks < 0) FAIL(FASTCOT_EINVAL, "%s: window or sinks below 0", name);
+    if (!a.r.B || !a.r.R || !a.r.n_rows) return 0;
+    if ((int64_t)a.r.n_rows * n_heads > 0x7FFFFFFF) FAIL(FASTCOT_ECAPACITY, "%s: more than 2^31 rows times heads", name);
+    if (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) FAIL(FASTCOT_EINVAL, "%s: queries and output have to be given, aligned to 16 bytes", name);
+    if (q_row_stride % 8 || q_head_stride % 8 || q_row_stride < 0 || q_head_stride < 0) FAIL(FASTCOT_EINVAL, "%s: strides of the queries are no multiples of 8", name);
+    if (out_row_stride % 8 || out_row_stride < (int64_t)n_heads * c->head_dim) FAIL(FASTCOT_EINVAL, "%s: row stride of the output below a row or no multiple of 8", name);
+    a.kl = a.c.k + (size_t)layer * c->n_pages * page_bytes(c);
+    a.vl = a.c.v + (size_t)layer * c->n_pages * page_bytes(c);
+    a.q = d_q; a.q_row = q_row_stride; a.q_head = q_head_stride;
+    a.out = d_out; a.out_row = out_row_stride; a.lse = d_lse;
+    a.H = n_heads; a.act = act_dtype; a.esz = (int32_t)esz_of(c); a.window = window; a.sinks = sinks;
+    a.cnt = (int32_t*)d_scratch + 64;
+    a.part = (float*)((char*)d_scratch + PG_HEAD + 3 * list_bytes(c));
+    return launched(name, fc_paged_attn(a, (hipStream_t)hip_stream));
+}
