@@ -45,8 +45,10 @@ struct PagedAttnArgs {
     void* out; int64_t out_row;
     float* lse;
     int32_t H, act;                        // act: 0 fp32, 1 bf16 rows
+    int32_t g; uint32_t g_inv;             // query heads of a K/V head, and 2^32 / g rounded up
     int32_t esz;                           // bytes of a cached value
     int32_t window, sinks;                 // window 0: none
+    int32_t whole;                         // most blocks of a unit that is not cut
     int32_t* cnt; float* part;             // hand-off of key splits: counters (zero between launches), partial results
 };
 size_t fc_paged_attn_scratch_bytes(int Dh);

@@ -3,8 +3,10 @@
 //
 //   s_k = q . k / sqrt(Dh),  m = max s_k,  l = sum e^(s_k - m),  out = sum e^(s_k - m) v_k / l,  lse = m + ln l
 //
-// A unit is 16 or 32 rows (token by token, the query heads of a K/V head next to each other) of one sequence and K/V head, a workgroup's work:
-// its waves take the visible blocks of 32 positions in turn, keep m, l and the sums in registers and meet in LDS.  Scores S^T = K . Q^T and
+// A unit is 16 or 32 rows (token by token, the query heads of a K/V head next to each other) of one sequence and K/V head.  The visible blocks of
+// 32 positions of all units, one after the other, are dealt to the launch's workgroups in equal parts (pg_deal): lengths come from device memory, so
+// a captured launch stays balanced while they move on.  A workgroup's waves take the blocks of its part of a unit in turn, keep m, l and the sums
+// in registers and meet in LDS; parts of one unit meet in memory, where the last workgroup to arrive joins them in order.  Scores S^T = K . Q^T and
 // sums O^T += V^T . P^T are matrix instructions whose operands lie in the cache as they are needed (k_index, v_index); for any head size
 // the 16-byte pieces u = 4 f + lane / 16 of a score tile's fragment f hold head elements 32 (u % G) + 8 (u / G) .. + 7, G = Dh / 32.
 // bf16 caches run on bf16 instructions with fp32 queries and weights in three parts (24 bits, so results are those of fp32 arithmetic) or bf16
@@ -12,7 +14,9 @@
 // Blocks that some row does not see whole are edges: their scores are masked, and V of positions that no row of the unit sees is taken as zero (a
 // weight of zero times an infinity is none).  Where V is not finite at a position that some rows see and others do not, the block's products
 // are summed position by position.
+#include "gemmco.h"      // fc_num_cus
 #include "paged.h"
+#include "xwg.h"
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
@@ -54,26 +58,237 @@ __device__ inline PagedRange pg_range(const PagedAttnArgs& a, int p0, int p1) {
     return r;
 }
 
+// One workgroup's part of a unit: blocks off .. off + len - 1 of its `blocks` visible ones
+struct PagedPart {
+    int b, kvh, tile;
+    int seq, n, first, rows;               // rows of the sequence times query heads of a K/V head
+    int off, len, blocks;
+    uint32_t base;                         // place of the unit's first block in what is dealt
+};
+struct PagedDeal { uint32_t share, at, end; };         // what a workgroup gets, and this one's places: at .. end - 1
+__device__ inline int pg_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// token of row x of a sequence: x / (query heads of a K/V head), x below 2^26
+__device__ inline int pg_token(const PagedAttnArgs& a, int x) { return a.g == 1 ? x : (int)__umulhi((uint32_t)x, a.g_inv); }
+// visible blocks of a tile of RT rows; rows of no sequence get one, that is not there
+template <int RT> __device__ inline int pg_blocks(const PagedAttnArgs& a, int seq, int n, int rows, int tile) {
+    if (tile * RT >= rows) return 0;
+    if (seq < 0) return 1;
+    const int last = tile * RT + RT < rows ? tile * RT + RT - 1 : rows - 1;
+    const PagedRange r = pg_range(a, n + pg_token(a, tile * RT), n + pg_token(a, last));
+    return r.sunk + r.hi - r.lo;
+}
+__device__ inline void pg_load(const PagedAttnArgs& a, int b, int& seq, int& n, int& first, int& rows) {
+    int count;
+    pg_rows(a.r, b, first, count);
+    seq = pg_seq(a.r, a.c, b);
+    n = seq < 0 ? 0 : pg_len(a.c, seq);
+    rows = count * a.g;
+}
+// inclusive prefix sum over the wave's lanes
+__device__ inline uint32_t pg_wave_scan(uint32_t x) {
+    int v = (int)x;
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);        // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);        // row_bcast 15, 31
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+    return (uint32_t)v;
+}
+__device__ inline uint32_t pg_lane(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+// What is dealt: PG_UNIT places for every unit and one for each of its blocks; units ordered by sequence, K/V head, tile.  Every workgroup gets an equal
+// share of at least PG_UNIT places, every wave finds its workgroup's by itself: lanes take sequences (or, where a sequence has more than four tiles,
+// tiles).  A unit of at most a.whole blocks is not cut, it belongs to the share that its first block falls into.  The host has checked that all
+// places fit 31 bits.  false: nothing for this worker.  p: the first part of its share.
+// A unit's queries, meeting and output take about as long as eight blocks: 48 sequences of 60 to 8100 positions over 40 heads take 302 us with 4 places a
+// unit, 256 with 8, 255 with 16; three short ones 10.9, 8.7 and 8.7 us, 200 of 20 to 300 positions over 8 heads 32.8, 32.9 and 35.3.
+#define PG_UNIT 8
+template <int RT> __device__ inline void pg_part(const PagedAttnArgs& a, PagedDeal& d, PagedPart& p) {     // the share's part of the unit p, from the place d.at on
+    if (p.blocks <= a.whole) { p.off = 0; p.len = p.base >= d.at && p.base < d.end ? p.blocks : 0; return; }
+    p.off = d.at > p.base ? (int)(d.at - p.base) : 0;
+    const int left = d.end > p.base ? (int)(d.end - p.base) : 0;           // places of the unit's blocks in front of the share's end
+    p.len = (left < p.blocks ? left : p.blocks) - p.off;
+}
+template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int tiles, int worker, int workers, PagedDeal& d, PagedPart& p) {
+    const int lane = threadIdx.x & 63, Hkv = a.c.Hkv;
+    const bool by_seq = tiles <= 4;
+    // places of one K/V head of sequence b in tiles t0 .. t1 - 1
+    auto places = [&](int b, int t0, int t1) -> uint32_t {
+        if (b >= a.r.B) return 0;
+        int seq, n, first, rows;
+        pg_load(a, b, seq, n, first, rows);
+        uint32_t s = 0;
+        for (int t = t0; t < t1; ++t) { const int x = pg_blocks<RT>(a, seq, n, rows, t); s += x ? x + PG_UNIT : 0; }
+        return s;
+    };
+    uint32_t total = 0, mine = 0, incl = 0;
+    if (by_seq) {
+        for (int b = 0; b < a.r.B; b += 64) { mine = places(b + lane, 0, tiles) * Hkv; incl = pg_wave_scan(mine); total += pg_lane(incl, 63); }
+    } else {
+        for (int b = 0; b < a.r.B; ++b) for (int t = 0; t < tiles; t += 64) mine += places(b, t + lane, t + lane + 1);
+        total = pg_lane(pg_wave_scan(mine), 63) * Hkv;
+    }
+    d.share = (total + workers - 1) / workers;
+    if (d.share < PG_UNIT) d.share = PG_UNIT;
+    d.at = d.share * worker;
+    if (d.at >= total) return false;
+    d.end = d.at + d.share < total ? d.at + d.share : total;
+    // the sequence that place d.at falls into, the places in front of it, and those of one of its heads
+    uint32_t before = 0, head = 0;
+    int b = 0;
+    if (by_seq) {
+        for (;; b += 64) {
+            if (a.r.B > 64) { mine = places(b + lane, 0, tiles) * Hkv; incl = pg_wave_scan(mine); }
+            const uint64_t hit = __ballot(before + incl > d.at);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                const uint32_t w = pg_lane(mine, l);
+                before += pg_lane(incl, l) - w;
+                head = w / Hkv;
+                b += l;
+                break;
+            }
+            before += pg_lane(incl, 63);
+        }
+    } else {
+        for (;; ++b) {
+            mine = 0;
+            for (int t = 0; t < tiles; t += 64) mine += places(b, t + lane, t + lane + 1);
+            head = pg_lane(pg_wave_scan(mine), 63);
+            if (before + head * Hkv > d.at) break;
+            before += head * Hkv;
+        }
+    }
+    p.b = b;
+    pg_load(a, b, p.seq, p.n, p.first, p.rows);
+    p.seq = pg_uniform(p.seq); p.n = pg_uniform(p.n); p.first = pg_uniform(p.first); p.rows = pg_uniform(p.rows);
+    p.kvh = pg_uniform((int)((d.at - before) / head));
+    before += head * p.kvh;
+    p.tile = 0;
+    if (by_seq) {
+        for (;; ++p.tile) {
+            p.blocks = pg_blocks<RT>(a, p.seq, p.n, p.rows, p.tile);
+            if (before + p.blocks + PG_UNIT > d.at) break;
+            before += p.blocks + PG_UNIT;
+        }
+    } else {
+        for (int t = 0;; t += 64) {
+            mine = pg_blocks<RT>(a, p.seq, p.n, p.rows, t + lane);
+            if (mine) mine += PG_UNIT;
+            incl = pg_wave_scan(mine);
+            const uint64_t hit = __ballot(before + incl > d.at);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                const uint32_t w = pg_lane(mine, l);
+                before += pg_lane(incl, l) - w;
+                p.blocks = (int)w - PG_UNIT;
+                p.tile = t + l;
+                break;
+            }
+            before += pg_lane(incl, 63);
+        }
+    }
+    p.blocks = pg_uniform(p.blocks); p.tile = pg_uniform(p.tile);
+    p.base = (uint32_t)pg_uniform((int)before) + PG_UNIT;
+    pg_part<RT>(a, d, p);
+    return true;
+}
+// the next part of the share (of which there may be nothing but places without a block)
+template <int RT> __device__ inline bool pg_next(const PagedAttnArgs& a, const PagedDeal& d, PagedPart& p) {
+    const uint32_t next = p.base + p.blocks;
+    if (next >= d.end) return false;
+    if (++p.tile * RT >= p.rows) {
+        p.tile = 0;
+        if (++p.kvh == a.c.Hkv) {
+            p.kvh = 0;
+            do {
+                ++p.b;
+                pg_load(a, p.b, p.seq, p.n, p.first, p.rows);
+                p.seq = pg_uniform(p.seq); p.n = pg_uniform(p.n); p.first = pg_uniform(p.first); p.rows = pg_uniform(p.rows);
+            } while (p.rows == 0);
+        }
+    }
+    p.blocks = pg_blocks<RT>(a, p.seq, p.n, p.rows, p.tile);
+    p.base = next + PG_UNIT;
+    PagedDeal e = d;
+    e.at = next;
+    pg_part<RT>(a, e, p);
+    return true;
+}
+// Where a part of a unit that several workgroups share keeps its results: a workgroup has at most two such parts, one that another one began (slot 0)
+// and one that another one ends.  Slots hold RT rows of Dh sums, then m and l of each row.
+
+// two joined sums of row x of a sequence to the output
+__device__ inline void pg_out(const PagedAttnArgs& a, int x, int first, int kvh, int Dh, int d, float M, float L, float o0, float o1) {
+    const int j = pg_token(a, x), row = first + j, h = kvh * a.g + x - j * a.g;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const size_t at = (size_t)row * a.out_row + (size_t)h * Dh + d;
+    if (a.act == FASTCOT_BF16) *(uint32_t*)((bf16_t*)a.out + at) = pk_bf16(o0 * inv, o1 * inv);
+    else *(float2*)((float*)a.out + at) = make_float2(o0 * inv, o1 * inv);
+    if (a.lse && d == 0) a.lse[(size_t)row * a.H + h] = (M == -INFINITY ? 0.f : M) * LN2 + logf(L);
+}
+// Joins the parts of a unit: a thread takes two sums of a row, of every part or, where that leaves threads idle, of every groups-th one; eight
+// parts are requested at a time.  (One after the other 32 parts took 15 us.)
+template <int G, int RT, int NW> __device__ inline void pg_join(const PagedAttnArgs& a, float* lds, int row0, int nrows, int first, int kvh, int w0, int parts) {
+    constexpr int Dh = 32 * G, SLOT = RT * (Dh + 2), T = NW * 64;
+    const int rows = nrows - row0 < RT ? nrows - row0 : RT, pairs = rows * (Dh / 2);
+    const float* p0 = a.part + (size_t)(2 * w0 + 1) * SLOT;    // the first part's slot; the others' are the even ones behind it
+    const int groups = pairs < T ? T / pairs : 1, grp = pairs < T ? (int)threadIdx.x / pairs : 0, y0 = pairs < T ? (int)threadIdx.x - grp * pairs : (int)threadIdx.x;
+    float M = -INFINITY, L = 0.f, o0 = 0.f, o1 = 0.f;
+    auto add = [&](float m, float l, float v0, float v1) {
+        const float Mn = fmaxf(M, m), Ms = Mn == -INFINITY ? 0.f : Mn;
+        const float x = __builtin_amdgcn_exp2f(M - Ms), w = __builtin_amdgcn_exp2f(m - Ms);
+        L = L * x + l * w; o0 = o0 * x + v0 * w; o1 = o1 * x + v1 * w;
+        M = Mn;
+    };
+    for (int y = y0; y < pairs && grp < groups; y += T) {
+        const int r = y / (Dh / 2), d = 2 * (y % (Dh / 2));
+        M = -INFINITY; L = o0 = o1 = 0.f;
+        for (int i0 = grp; i0 < parts; i0 += 8 * groups) {
+            float m[8], l[8], v0[8], v1[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = i0 + e * groups < parts ? i0 + e * groups : i0;
+                const float* s = p0 + (i ? (size_t)(2 * i - 1) * SLOT : 0);
+                ld_agent_f32x2(s + RT * Dh + 2 * r, m[e], l[e]);
+                ld_agent_f32x2(s + r * Dh + d, v0[e], v1[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (i0 + e * groups < parts) add(m[e], l[e], v0[e], v1[e]);
+        }
+        if (groups == 1) pg_out(a, row0 + r, first, kvh, Dh, d, M, L, o0, o1);
+    }
+    if (groups > 1) {
+        if (grp < groups) *(float4*)(lds + 4 * threadIdx.x) = make_float4(M, L, o0, o1);
+        __syncthreads();
+        if ((int)threadIdx.x < pairs) {
+            for (int k = 1; k < groups; ++k) { const float4 z = *(const float4*)(lds + 4 * (threadIdx.x + k * pairs)); add(z.x, z.y, z.z, z.w); }
+            pg_out(a, row0 + y0 / (Dh / 2), first, kvh, Dh, 2 * (y0 % (Dh / 2)), M, L, o0, o1);
+        }
+    }
+}
+
 // G: 32s of a head; F32: fp32 cache; QT: tiles of 16 rows of a unit; NW: waves; QP, PP: bf16 parts of queries and weights
 template <int G, bool F32, int QT, int NW, int QP, int PP>
 __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int tiles) {
     constexpr int Dh = 32 * G, NV = 2 * G, RT = 16 * QT;       // NV: fragments of V, four sums of a lane each
     constexpr int PART = Dh * 16 + 32;                         // floats of a wave's tile: sums, then m and l of the 16 rows
     extern __shared__ float lds[];
+    __shared__ int arrived;
     const int lane = threadIdx.x & 63, lm = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = blockIdx.x % tiles, kvh = blockIdx.x / tiles % a.c.Hkv, b = blockIdx.x / tiles / a.c.Hkv;
-    const int g = a.H / a.c.Hkv;
-    int first, count;
-    pg_rows(a.r, b, first, count);
-    const int row0 = tile * RT, nrows = count * g;             // rows of the unit: row0 .. of nrows, row x = head x % g of token x / g
-    if (row0 >= nrows) return;
-    const int seq = pg_seq(a.r, a.c, b), n = seq < 0 ? 0 : pg_len(a.c, seq);
-    const int j0 = row0 / g, last = row0 + RT < nrows ? row0 + RT - 1 : nrows - 1, j1 = last / g;
+    PagedDeal deal;
+    PagedPart part;
+    if (!pg_deal<RT>(a, tiles, blockIdx.x, gridDim.x, deal, part)) return;
+  do {
+    if (part.len <= 0) continue;                               // (a share that ends in front of the unit's first block)
+    const int kvh = part.kvh, first = part.first, nrows = part.rows, seq = part.seq, n = part.n;
+    const int row0 = part.tile * RT;                           // rows of the unit: row0 .. of nrows, row x = head x % g of token x / g
+    const int g = a.g, last = row0 + RT < nrows ? row0 + RT - 1 : nrows - 1;
+    const int j0 = pg_token(a, row0), j1 = pg_token(a, last);
     const int p0 = n + j0, p1 = n + j1;
     const PagedRange vis = pg_range(a, p0, p1);
     const int* table = a.c.table + (size_t)(seq < 0 ? 0 : seq) * a.c.MP;
-    const int blocks = seq < 0 ? 0 : vis.sunk + vis.hi - vis.lo;
     const float scale2 = LOG2E / sqrtf((float)Dh);             // the softmax runs in powers of two
 
     int pos[QT];                                               // this lane's rows: row row0 + 16 * qt + lm (-1: none)
@@ -81,9 +296,9 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
     float qx[F32 ? QT : 1][G][8];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        const int x = row0 + 16 * qt + lm, row = x < nrows ? x : last, j = row / g;
+        const int x = row0 + 16 * qt + lm, row = x < nrows ? x : last, j = pg_token(a, row);
         pos[qt] = x < nrows ? n + j : -1;
-        const size_t at = (size_t)(first + j) * a.q_row + (size_t)(kvh * g + row % g) * a.q_head;
+        const size_t at = (size_t)(first + j) * a.q_row + (size_t)(kvh * g + row - j * g) * a.q_head;
 #pragma unroll
         for (int f = 0; f < G; ++f) {
             const int u = 4 * f + lg, dh = 32 * (u % G) + 8 * (u / G);
@@ -109,10 +324,10 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
         for (int f = 0; f < NV; ++f) acc[qt][f] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int x = wv; x < blocks; x += NW) {
+    for (int x = part.off + wv; x < part.off + part.len; x += NW) {
         const int blk = x < vis.sunk ? x : x - vis.sunk + vis.lo, kb = blk << 5;
         const int slot = blk >> a.c.pb;
-        const int page = slot < a.c.MP ? table[slot] : -1;
+        const int page = slot < a.c.MP && seq >= 0 ? table[slot] : -1;
         if (page < 0 || page >= a.c.N) continue;
         const size_t at = ((((size_t)page * a.c.Hkv + kvh) << a.c.pb) + (blk & ((1 << a.c.pb) - 1))) * 32 * Dh;
         constexpr int FW = F32 ? 2 : 1;                        // 16-byte words of a lane's eight values
@@ -231,6 +446,8 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
         if (lg == 0) { dst[Dh * 16 + lm] = m[qt]; dst[Dh * 16 + 16 + lm] = l[qt]; }
     }
     __syncthreads();
+    const bool shared = part.len < part.blocks;
+    float* mine = a.part + (size_t)(2 * blockIdx.x + (part.off == 0)) * RT * (Dh + 2);
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int x = row0 + 16 * qt + lm;
@@ -240,8 +457,8 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
         const float Ms = M == -INFINITY ? 0.f : M;
 #pragma unroll
         for (int i = 0; i < NW; ++i) { w[i] = __builtin_amdgcn_exp2f(w[i] - Ms); L += lds[(i * QT + qt) * PART + Dh * 16 + 16 + lm] * w[i]; }
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        const int row = first + x / g, h = kvh * g + x % g;
+        const float inv = shared ? 1.f : L == 0.f ? 0.f : 1.f / L;
+        const int j = pg_token(a, x), row = first + j, h = kvh * g + x - j * g;
         for (int f = wv; f < NV; f += NW) {
             f32x4_t o = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -249,34 +466,67 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
                 const f32x4_t y = *(const f32x4_t*)(lds + (i * QT + qt) * PART + (f * 64 + lane) * 4);
                 o += y * w[i];
             }
-            o *= inv;
             if (x >= nrows) continue;
+            if (shared) {
+                float* to = mine + (16 * qt + lm) * Dh + 16 * f + 4 * lg;
+                st_agent_f32x2(to, o[0], o[1]);
+                st_agent_f32x2(to + 2, o[2], o[3]);
+                continue;
+            }
+            o *= inv;
             const size_t at = (size_t)row * a.out_row + (size_t)h * Dh + 16 * f + 4 * lg;
             if (a.act == FASTCOT_BF16) *(uint2*)((bf16_t*)a.out + at) = make_uint2(pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3]));
             else *(f32x4_t*)((float*)a.out + at) = o;
         }
-        if (a.lse && wv == 0 && lg == 0 && x < nrows) a.lse[(size_t)row * a.H + h] = Ms * LN2 + logf(L);
+        if (wv == 0 && lg == 0 && x < nrows) {
+            if (shared) st_agent_f32x2(mine + RT * Dh + 2 * (16 * qt + lm), M, L);
+            else if (a.lse) a.lse[(size_t)row * a.H + h] = Ms * LN2 + logf(L);
+        }
     }
+    if (shared) {
+        wait_vmem_done();
+        __syncthreads();
+        const int w0 = (int)(part.base / deal.share), parts = (int)((part.base + part.blocks - 1) / deal.share) - w0 + 1;
+        if (threadIdx.x == 0) arrived = arrive_agent(a.cnt + w0);
+        __syncthreads();
+        if (arrived == parts - 1) {
+            pg_join<G, RT, NW>(a, lds, row0, nrows, first, kvh, w0, parts);
+            if (threadIdx.x == 0) st_agent_i32(a.cnt + w0, 0);
+        }
+    }
+    __syncthreads();                                           // (the LDS is written again)
+  } while (pg_next<RT>(a, deal, part));
 }
 
-size_t fc_paged_attn_scratch_bytes(int Dh) { return 0 * Dh; }
+#define PG_WORKERS 1024          // most workgroups of a launch
+// partial results: two slots a workgroup, of up to 32 rows
+size_t fc_paged_attn_scratch_bytes(int Dh) { return (size_t)PG_WORKERS * 2 * 32 * (Dh + 2) * 4; }
 
+template <int G, bool F32, int QT, int NW, int QP, int PP>
+static hipError_t launch_as(PagedAttnArgs a, int grid, hipStream_t st) {
+    const int rows = a.r.R * a.g;
+    const size_t bytes = (size_t)NW * QT * (32 * G * 16 + 32) * 4;
+    auto kernel = k_paged_attn<G, F32, QT, NW, QP, PP>;
+    // (more than 64 KB of LDS have to be asked for)
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return e;
+    a.whole = 4 * NW;          // blocks of a unit that is not cut: four rounds of its waves take about as long as a meeting in memory
+    kernel<<<grid < PG_WORKERS ? grid : PG_WORKERS, NW * 64, bytes, st>>>(a, (rows + 16 * QT - 1) / (16 * QT));
+    return hipGetLastError();
+}
+// Up to 16 rows: where every unit finds a CU of its own, eight waves share its blocks; with more units two workgroups of four waves on every CU, so that
+// one's loads go on while the other one's waves meet (32 sequences of 100 to 500 positions over 32 heads 36.7 / 31.3 us, 200 of 20 to 300 over 8 heads
+// 41.7 / 32.9; the other way round 7B heads, 8000 positions 26.5 / 26.8, 70B heads, 120000 positions 88 / 100, 7B window of 16, 777 positions 13.3 / 15.8).
+// Heads of more than 128 elements and two tiles need the registers of a CU for four waves.
 template <int G, bool F32, int QP, int PP>
 static hipError_t launch(const PagedAttnArgs& a, hipStream_t st) {
-    constexpr int NW = G <= 4 ? 8 : 4;
-    const int rows = a.r.R * (a.H / a.c.Hkv);
-    const bool two = rows > 16;
-    const int tiles = (rows + (two ? 31 : 15)) / (two ? 32 : 16);
-    const unsigned grid = (unsigned)(tiles * a.c.Hkv) * (unsigned)a.r.B;
-    const size_t bytes = (size_t)NW * (two ? 2 : 1) * (32 * G * 16 + 32) * 4;
-    auto one = k_paged_attn<G, F32, 1, NW, QP, PP>;
-    auto pair = k_paged_attn<G, F32, 2, NW, QP, PP>;
-    // (more than 64 KB of LDS have to be asked for)
-    const hipError_t e = hipFuncSetAttribute((const void*)(two ? pair : one), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e != hipSuccess) return e;
-    if (two) pair<<<grid, NW * 64, bytes, st>>>(a, tiles);
-    else one<<<grid, NW * 64, bytes, st>>>(a, tiles);
-    return hipGetLastError();
+    const int cus = fc_num_cus();
+    if (a.r.R * a.g > 16) return launch_as<G, F32, 2, 4, QP, PP>(a, cus, st);
+    if constexpr (G <= 4) {
+        if ((int64_t)a.r.B * a.c.Hkv <= cus) return launch_as<G, F32, 1, 8, QP, PP>(a, cus, st);
+        return launch_as<G, F32, 1, 4, QP, PP>(a, 2 * cus, st);
+    }
+    return launch_as<G, F32, 1, 4, QP, PP>(a, cus, st);
 }
 template <int G> static hipError_t by_type(const PagedAttnArgs& a, hipStream_t st) {
     if (a.esz == 4) return launch<G, true, 1, 1>(a, st);

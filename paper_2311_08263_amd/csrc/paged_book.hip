@@ -492,7 +492,10 @@ extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const f
     if (n_heads < 1 || n_heads % c->n_kv_heads || n_heads / c->n_kv_heads > 64) FAIL(FASTCOT_EINVAL, "%s: heads are no multiple (up to 64) of the cache's", name);
     if (window < 0 || sinks < 0) FAIL(FASTCOT_EINVAL, "%s: window or sinks below 0", name);
     if (!a.r.B || !a.r.R || !a.r.n_rows) return 0;
-    if ((int64_t)a.r.n_rows * n_heads > 0x7FFFFFFF) FAIL(FASTCOT_ECAPACITY, "%s: more than 2^31 rows times heads", name);
+    // (what the kernel deals to its workgroups: blocks of 32 positions, and some more, for every 16 rows of a K/V head)
+    const double g = n_heads / c->n_kv_heads, tiles = (a.r.R * g + 15) / 16, blocks = (double)c->max_pages * (c->page_size / 32) + a.r.R / 32 + 10;
+    if (a.r.R * g >= (1 << 26) || (double)a.r.B * c->n_kv_heads * tiles * blocks >= 2147483648.0)
+        FAIL(FASTCOT_ECAPACITY, "%s: rows times positions of the table pass 2^31 blocks", name);
     if (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) FAIL(FASTCOT_EINVAL, "%s: queries and output have to be given, aligned to 16 bytes", name);
     if (q_row_stride % 8 || q_head_stride % 8 || q_row_stride < 0 || q_head_stride < 0) FAIL(FASTCOT_EINVAL, "%s: strides of the queries are no multiples of 8", name);
     if (out_row_stride % 8 || out_row_stride < (int64_t)n_heads * c->head_dim) FAIL(FASTCOT_EINVAL, "%s: row stride of the output below a row or no multiple of 8", name);
@@ -500,7 +503,7 @@ extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const f
     a.vl = a.c.v + (size_t)layer * c->n_pages * page_bytes(c);
     a.q = d_q; a.q_row = q_row_stride; a.q_head = q_head_stride;
     a.out = d_out; a.out_row = out_row_stride; a.lse = d_lse;
-    a.H = n_heads; a.act = act_dtype; a.esz = (int32_t)esz_of(c); a.window = window; a.sinks = sinks;
+    a.H = n_heads; a.act = act_dtype; a.g = n_heads / c->n_kv_heads; a.g_inv = (uint32_t)(((1ull << 32) + a.g - 1) / a.g); a.esz = (int32_t)esz_of(c); a.window = window; a.sinks = sinks;
     a.cnt = (int32_t*)d_scratch + 64;
     a.part = (float*)((char*)d_scratch + PG_HEAD + 3 * list_bytes(c));
     return launched(name, fc_paged_attn(a, (hipStream_t)hip_stream));

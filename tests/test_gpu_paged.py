@@ -334,3 +334,53 @@ def test_serving_loop(fc):
         torch.cuda.synchronize()
         assert rel(parts["out"], want) < 2e-6
         plain.same(c)
+
+
+@pytest.mark.parametrize("B,lo,hi,rows,H,Hkv,Dh,P,cache,act,window,sinks", [
+    (1, 5000, 5000, 1, 8, 1, 128, 64, "bf16", "bf16", 0, 0),             # many parts of one unit
+    (1, 3001, 3001, 9, 4, 2, 64, 32, "f32", "f32", 0, 0),
+    (70, 0, 900, 1, 4, 4, 128, 32, "bf16", "f32", 0, 0),                 # more sequences than lanes, parts that begin and end inside units
+    (130, 0, 400, 3, 2, 1, 32, 32, "bf16", "f32", 100, 2),
+    (5, 100, 3000, 7, 16, 2, 96, 128, "bf16", "bf16", 700, 40),
+    (3, 10, 2000, 300, 4, 2, 128, 64, "bf16", "f32", 0, 0),              # more than four tiles of a sequence
+    (2, 700, 1500, 90, 16, 1, 64, 64, "bf16", "bf16", 333, 7),
+    (2, 10, 1000, 130, 4, 4, 256, 64, "f32", "f32", 0, 0),
+])
+def test_attention_in_parts(fc, B, lo, hi, rows, H, Hkv, Dh, P, cache, act, window, sinks):
+    """Units that several workgroups share, joined in memory: the same bits in every call, and a scratch that is as it was afterwards."""
+    import torch
+    say(f"paged attention in parts B={B} {lo}..{hi} rows={rows} H={H}/{Hkv} Dh={Dh} {cache} {act} window={window}")
+    rnd = random.Random(B)
+    lens = [rnd.randint(lo, hi) for _ in range(B)]
+    n_rows = [rows] * B if B < 3 else [rnd.randint(0, rows) for _ in range(B - 1)] + [rows]
+    c, slots = make(fc, lens, n_rows, P, Hkv, Dh, cache)
+    q = queries(n_rows, H, Dh, act)
+    where = dict(seqs=ints(slots), row_start=starts(n_rows), max_rows=rows, window=window, sinks=sinks, want_lse=True)
+    out, lse = c.attn(q, **where)
+    check(out, lse, dense(c, slots, n_rows, q, window, sinks), act)
+    for _ in range(3):
+        again, lse2 = c.attn(q, **where)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+def dense(c, slots, rows, q, window, sinks):
+    """Plain.attn with a matrix for each sequence and head."""
+    import torch
+    Dh, P = q.shape[2], c._desc.page_size
+    kc, vc = canonical(c.k, Dh)[0][0], canonical(c.v, Dh)[1][0]
+    H, G = q.shape[1], q.shape[1] // kc.shape[1]
+    out, lse, x = torch.zeros(sum(rows), H, Dh, dtype=torch.float64, device="cuda"), torch.zeros(sum(rows), H, dtype=torch.float64, device="cuda"), 0
+    for s, r in zip(slots, rows):
+        n = int(c.len[s])
+        key, pos = torch.arange(n + r, device="cuda"), torch.arange(n, n + r, device="cuda")[:, None]
+        pages = c.table[s].long()[key // P]
+        hidden = (key > pos) | (pages < 0)
+        if window:
+            hidden |= (key <= pos - window) & (key >= sinks)
+        for h in range(H if r else 0):
+            k, v = (x_[pages.clamp(min=0), h // G, key % P].double() for x_ in (kc, vc))
+            score = (q[x:x + r, h].double() @ k.T / Dh ** 0.5).masked_fill(hidden, -torch.inf)
+            lse[x:x + r, h] = torch.logsumexp(score, 1)
+            out[x:x + r, h] = torch.softmax(score, 1) @ v
+        x += r
+    return out.view(sum(rows), -1), lse
