@@ -26,6 +26,7 @@ typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
 #define LN2 0.6931471805599453f
 
 // The parts of a fp32 value are cut off its bits from the top, so that none overflows and three hold all 24 bits
+// (one or two: the last one is rounded)
 template <int TERMS> __device__ inline void pg_split8(const float* v, u32x4_t* part) {
     float x[8];
 #pragma unroll
@@ -36,15 +37,60 @@ template <int TERMS> __device__ inline void pg_split8(const float* v, u32x4_t* p
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t a = __float_as_uint(x[2 * e]), b = __float_as_uint(x[2 * e + 1]);
-            if (t == TERMS - 1 && TERMS < 3) w[e] = pk_bf16(x[2 * e], x[2 * e + 1]);          // the last of fewer parts is rounded
+            if (t == TERMS - 1 && TERMS < 3) w[e] = pk_bf16(x[2 * e], x[2 * e + 1]);
             else w[e] = (a >> 16) | (b & 0xFFFF0000u);
             if (t < TERMS - 1) { x[2 * e] -= __uint_as_float(a & 0xFFFF0000u); x[2 * e + 1] -= __uint_as_float(b & 0xFFFF0000u); }
         }
         part[t] = (u32x4_t){w[0], w[1], w[2], w[3]};
     }
 }
+#define ROW_NONE (-3.0e38f)      // reference of a row that has seen nothing
+// Products p become the exponents by * p - from, each operation rounded: where the reference is far from zero a product as large as the largest one has to
+// give an exponent of zero, which a fused multiply-add with the rounded reference does not
+__device__ inline void pg_far(float* p, float& by, float& from) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = p[e] * by - from;
+    by = 1.f; from = 0.f;
+}
 __device__ inline bool pg_sees(const PagedAttnArgs& a, int key, int pos) {
     return key <= pos && (!a.window || key > pos - a.window || key < a.sinks);
+}
+// Eight bf16 values of V: zero outside `keep`, and zero where they are not finite; whether any of those kept is not.  (An infinity or NaN is added by itself to
+// the rows that see it, whatever its weight: multiplied by a weight of zero it would reach the others.)
+__device__ inline bool pg_finite(u32x4_t& v, const uint32_t* keep) {
+    uint32_t found = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t x = v[w] & keep[w], bad = ((x & 0x7F80u) == 0x7F80u ? 0x0000FFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+        v[w] = x & ~bad;
+        found |= bad;
+    }
+    return found != 0;
+}
+// What is not finite among eight values of V: ones where it is +infinity or NaN, and where it is -infinity or NaN
+__device__ inline void pg_infinite(u32x4_t& up, u32x4_t& down) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t x = up[w], lo = x & 0xFFFFu, hi = x >> 16;
+        auto one = [](uint32_t b, uint32_t sign) { return (b & 0x7FFFu) > 0x7F80u || b == (sign | 0x7F80u) ? 0x3F80u : 0u; };
+        up[w] = one(lo, 0u) | one(hi, 0u) << 16;
+        down[w] = one(lo, 0x8000u) | one(hi, 0x8000u) << 16;
+    }
+}
+// ones where a row at position pos sees position key, key + 1, .. key + 7
+__device__ inline u32x4_t pg_seen8(const PagedAttnArgs& a, int key, int pos) {
+    u32x4_t r;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) r[w] = (pg_sees(a, key + 2 * w, pos) ? 0x3F80u : 0u) | (pg_sees(a, key + 2 * w + 1, pos) ? 0x3F800000u : 0u);
+    return r;
+}
+__device__ inline void pg_add_infinite(f32x4_t& acc, const u32x4_t& up, const u32x4_t& down, const u32x4_t& seen) {
+    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+    const f32x4_t x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, up), __builtin_bit_cast(bf16x8_t, seen), zero, 0, 0, 0);
+    const f32x4_t y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, down), __builtin_bit_cast(bf16x8_t, seen), zero, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += (x[i] > 0.f ? INFINITY : 0.f) + (y[i] > 0.f ? -INFINITY : 0.f);
 }
 // the blocks of 32 positions that rows at positions p0 .. p1 see: the first `sunk`, then lo .. hi - 1
 struct PagedRange { int sunk, lo, hi; };
@@ -67,6 +113,14 @@ struct PagedPart {
 };
 struct PagedDeal { uint32_t share, at, end; };         // what a workgroup gets, and this one's places: at .. end - 1
 __device__ inline int pg_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// a structure of 32-bit words that is the same in every lane
+template <class T> __device__ inline T pg_uniform(const T& x) {
+    T y = x;
+    int* w = (int*)&y;
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 4; ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+    return y;
+}
 // token of row x of a sequence: x / (query heads of a K/V head), x below 2^26
 __device__ inline int pg_token(const PagedAttnArgs& a, int x) { return a.g == 1 ? x : (int)__umulhi((uint32_t)x, a.g_inv); }
 // visible blocks of a tile of RT rows; rows of no sequence get one, that is not there
@@ -273,7 +327,7 @@ template <int G, bool F32, int QT, int NW, int QP, int PP>
 __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int tiles) {
     constexpr int Dh = 32 * G, NV = 2 * G, RT = 16 * QT;       // NV: fragments of V, four sums of a lane each
     constexpr int PART = Dh * 16 + 32;                         // floats of a wave's tile: sums, then m and l of the 16 rows
-    extern __shared__ float lds[];
+    extern __shared__ __align__(16) float lds[];
     __shared__ int arrived;
     const int lane = threadIdx.x & 63, lm = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -498,9 +552,283 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
   } while (pg_next<RT>(a, deal, part));
 }
 
-#define PG_WORKERS 1024          // most workgroups of a launch
-// partial results: two slots a workgroup, of up to 32 rows
-size_t fc_paged_attn_scratch_bytes(int Dh) { return (size_t)PG_WORKERS * 2 * 32 * (Dh + 2) * 4; }
+// Many rows of a sequence (prompt chunks, wide windows, windows over grouped heads; bf16 caches): 64 * QT rows a unit.  Four waves of 16 * QT rows take the even
+// blocks, four with the same rows the odd ones; a pair of blocks goes global -> LDS while the previous pair is used, so that K and V are
+// read once for all the unit's rows and a fragment from LDS once for a wave's QT tiles.  At the end the two waves of the same rows exchange half of their sums.
+// Bound: matrix instructions (16 of 16 x 16 x 32 for a tile and block with bf16 rows, 48 with fp32 rows) beside about 30 vector instructions and 8
+// exponentials for bf16 rows.  To keep those few, sums are taken relative to a reference that moves only when a score passes it by 8 powers of two (so
+// weights are at most 2^8, and nothing is rescaled in most blocks).  With bf16 rows the weights are rounded to bf16 once in front of the product
+// with V: as large an error as the rounding of the output, half a step of each weight; their sum is taken before the rounding.
+template <int G, int QT, int QP, int PP>
+__global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tiles) {
+    constexpr int Dh = 32 * G, NV = 2 * G, RT = 64 * QT, SEC = 128 * G;    // SEC: 16-byte words of one block of K or V
+    extern __shared__ __align__(16) float lds[];
+    __shared__ int arrived;
+    __shared__ PagedPart kept_part;
+    __shared__ PagedDeal kept_deal;
+    __shared__ int bad[2][2];
+    u32x4_t* kv = (u32x4_t*)lds;                               // [buffer][block of the pair][K, V][SEC]
+    const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lg = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv >> 2, rg = wv & 3;
+    // consecutive shares on one XCD: units of one K/V head follow each other and find its blocks in that L2
+    const int per = gridDim.x >> 3, worker = gridDim.x & 7 ? blockIdx.x : (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    PagedDeal deal;
+    PagedPart part;
+    if (!pg_deal<RT>(a, tiles, worker, gridDim.x, deal, part)) return;
+    const float scale2 = LOG2E / sqrtf((float)Dh);
+    const float unscaled = QP == 1 ? scale2 : 1.f;             // what turns a product into an exponent of two
+  do {
+    if (part.len <= 0) continue;
+    const int kvh = part.kvh, first = part.first, nrows = part.rows, seq = part.seq, n = part.n, g = a.g;
+    const int row0 = part.tile * RT, r0 = row0 + 16 * QT * rg; // the unit's rows, this wave's
+    const int last = row0 + RT < nrows ? row0 + RT - 1 : nrows - 1;
+    const PagedRange vis = pg_range(a, n + pg_token(a, row0), n + pg_token(a, last));
+    const int plast = n + pg_token(a, last);
+    const bool any_rows = r0 < nrows;
+    const int lastw = r0 + 16 * QT < nrows ? r0 + 16 * QT - 1 : nrows - 1;
+    const int p0 = n + pg_token(a, any_rows ? r0 : lastw), p1 = n + pg_token(a, lastw);        // positions of the wave's rows
+    const int* table = a.c.table + (size_t)(seq < 0 ? 0 : seq) * a.c.MP;
+    const int end = part.off + part.len;
+
+    int pos[QT];
+    u32x4_t qf[QT][G][QP];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        const int x = r0 + 16 * qt + lm, row = x < nrows ? x : nrows - 1, j = pg_token(a, row);
+        pos[qt] = x < nrows ? n + j : -1;
+        const size_t at = (size_t)(first + j) * a.q_row + (size_t)(kvh * g + row - j * g) * a.q_head;
+#pragma unroll
+        for (int f = 0; f < G; ++f) {
+            const int u = 4 * f + lg, dh = 32 * (u % G) + 8 * (u / G);
+            if constexpr (QP == 1) qf[qt][f][0] = *(const u32x4_t*)((const bf16_t*)a.q + at + dh);
+            else {
+                const float4 y = *(const float4*)((const float*)a.q + at + dh), z = *(const float4*)((const float*)a.q + at + dh + 4);
+                const float v[8] = {y.x * scale2, y.y * scale2, y.z * scale2, y.w * scale2, z.x * scale2, z.y * scale2, z.z * scale2, z.w * scale2};
+                pg_split8<QP>(v, qf[qt][f]);
+            }
+        }
+    }
+    f32x4_t acc[QT][NV];
+    float R[QT], l[QT];                                        // reference of the row's exponents, this lane's share of the sum of weights
+    bool far = false;                                          // some reference is far from zero
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        R[qt] = ROW_NONE; l[qt] = 0.f;
+#pragma unroll
+        for (int f = 0; f < NV; ++f) acc[qt][f] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+
+    // pages of 64 blocks of the part at a time, one a lane: those at hand and the next ones (-1: no page, the block is not used)
+    auto pages_from = [&](int x0) {
+        const int x = x0 + lane, blk = x < vis.sunk ? x : x - vis.sunk + vis.lo, slot = blk >> a.c.pb;
+        const int page = seq >= 0 && x < end && slot < a.c.MP ? table[slot] : -1;
+        return page >= 0 && page < a.c.N ? page : -1;
+    };
+    int now = pages_from(part.off), next = pages_from(part.off + 64), held = part.off;         // held: the first block of those at hand
+    const int inpage = (1 << a.c.pb) - 1;
+    u32x4_t stage[G];
+    // requests the pair of blocks x, x + 1, whose pages become page0 and page1
+    int page0, page1;
+    auto load = [&](int x) {
+        if (x - held == 64) { held += 64; now = next; next = pages_from(held + 64); }
+        page0 = __builtin_amdgcn_readlane(now, x - held);
+        page1 = __builtin_amdgcn_readlane(now, x + 1 - held);
+        const int b0 = x < vis.sunk ? x : x - vis.sunk + vis.lo, b1 = x + 1 < vis.sunk ? x + 1 : x + 1 - vis.sunk + vis.lo;
+        const size_t at0 = ((((size_t)(page0 < 0 ? 0 : page0) * a.c.Hkv + kvh) << a.c.pb) + (b0 & inpage)) * SEC;
+        const size_t at1 = ((((size_t)(page1 < 0 ? 0 : page1) * a.c.Hkv + kvh) << a.c.pb) + (b1 & inpage)) * SEC;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int w0 = i * 512 + wv * 64, sec = G == 4 ? i : w0 / SEC;         // sec: block of the pair, K or V
+            stage[i] = *((const u32x4_t*)(sec & 1 ? a.vl : a.kl) + (sec & 2 ? at1 : at0) + (w0 - sec * SEC) + lane);
+        }
+    };
+    // puts the pair of blocks x, x + 1 into a buffer.  V goes in with zeros for what is not finite, and where the unit's last row does not see it: a weight of zero
+    // times an infinity would be none.  Of what is not finite and seen `bad` keeps the pair's number; it is added by itself to the rows that see it
+    auto store = [&](int buf, int x) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int w0 = i * 512 + wv * 64, sec = G == 4 ? i : w0 / SEC;
+            u32x4_t v = stage[i];
+            if (sec & 1) {
+                const int y = x + (sec >> 1), kb = (y < vis.sunk ? y : y - vis.sunk + vis.lo) << 5;
+                uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+                if (kb + 31 > plast) {
+                    const int past = kb + 8 * lg;              // the positions of this lane's eight values
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) keep[w] = (past + 2 * w <= plast ? 0x0000FFFFu : 0u) | (past + 2 * w + 1 <= plast ? 0xFFFF0000u : 0u);
+                }
+                if (pg_finite(v, keep)) bad[buf][sec >> 1] = x;
+            }
+            kv[buf * 4 * SEC + i * 512 + tid] = v;
+        }
+    };
+
+    auto compute = [&](const u32x4_t* kb_lds, int kb, bool whole) {
+        const u32x4_t* vb_lds = kb_lds + SEC;
+        f32x4_t sc[QT][2];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) sc[qt][0] = sc[qt][1] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+        // (fragments are read all at once, those of V in front of the softmax: one by one, in front of their instructions, each is a wait)
+        u32x4_t kf[2 * G], vf[NV];
+#pragma unroll
+        for (int f = 0; f < 2 * G; ++f) kf[f] = kb_lds[f * 64 + lane];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int f = 0; f < G; ++f) {
+                const bf16x8_t k = __builtin_bit_cast(bf16x8_t, kf[t * G + f]);
+#pragma unroll
+                for (int q = QP - 1; q >= 0; --q)
+#pragma unroll
+                    for (int qt = 0; qt < QT; ++qt) sc[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8_t, qf[qt][f][q]), sc[qt][t], 0, 0, 0);
+            }
+#pragma unroll
+        for (int f = 0; f < NV; ++f) vf[f] = vb_lds[f * 64 + lane];
+        __builtin_amdgcn_sched_barrier(0);
+        u32x4_t pf[QT][PP];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            float p[8], top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = sc[qt][e >> 2][e & 3];
+            if (!whole) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = pg_sees(a, kb + 8 * lg + e, pos[qt]) ? p[e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, p[e]);
+            float by = unscaled, from = R[qt];                 // weights are 2^(by * p - from)
+            if (__any(by * top > from + 8.f)) {
+                top *= by;
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float Rn = fmaxf(R[qt], top), alpha = __builtin_amdgcn_exp2f(R[qt] - Rn);
+                R[qt] = from = Rn;
+                far = far || __any(Rn > 1048576.f || (Rn < -1048576.f && Rn > ROW_NONE));
+                l[qt] *= alpha;
+#pragma unroll
+                for (int f = 0; f < NV; ++f) acc[qt][f] *= alpha;
+            }
+            if (QP == 1 && far) pg_far(p, by, from);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], by, -from)); l[qt] += p[e]; }
+            pg_split8<PP>(p, pf[qt]);
+        }
+#pragma unroll
+        for (int f = 0; f < NV; ++f) {
+            const bf16x8_t v = __builtin_bit_cast(bf16x8_t, vf[f]);
+#pragma unroll
+            for (int q = PP - 1; q >= 0; --q)
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt) acc[qt][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, pf[qt][q]), acc[qt][f], 0, 0, 0);
+        }
+    };
+    // what is not finite in V of block blk of a page, for the rows that see it
+    auto add_infinite = [&](int blk, int page) {
+        const u32x4_t* v = (const u32x4_t*)a.vl + ((((size_t)page * a.c.Hkv + kvh) << a.c.pb) + (blk & inpage)) * SEC + lane;
+        u32x4_t sees[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) sees[qt] = pg_seen8(a, (blk << 5) + 8 * lg, pos[qt]);
+#pragma unroll
+        for (int f = 0; f < NV; ++f) {
+            u32x4_t up = v[f * 64], down;
+            pg_infinite(up, down);
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) pg_add_infinite(acc[qt][f], up, down, sees[qt]);
+        }
+    };
+
+    if (tid < 4) bad[tid >> 1][tid & 1] = -1;
+    if (tid == 0) { kept_part = part; kept_deal = deal; }      // (scalar registers are short in the walk)
+    load(part.off);
+    __syncthreads();
+    store(0, part.off);
+    __syncthreads();
+    int buf = 0;
+    for (int x = part.off; x < end; x += 2) {
+        const int blk = x + kg < vis.sunk ? x + kg : x + kg - vis.sunk + vis.lo, kb = blk << 5, page = kg ? page1 : page0;
+        if (x + 2 < end) load(x + 2);                          // travels while this pair is used
+        __builtin_amdgcn_sched_barrier(0);
+        // does any row of the wave see the block, and do all of them see all of it
+        const bool seen = any_rows && page >= 0 && kb <= p1 && (!a.window || kb + 31 > p0 - a.window || kb < a.sinks);
+        const bool whole = kb + 31 <= p0 && (!a.window || kb > p1 - a.window || kb + 31 < a.sinks);
+        if (seen) {
+            const u32x4_t* at = kv + (buf * 4 + 2 * kg) * SEC;
+            compute(at, kb, whole);
+            if (bad[buf][kg] == x) add_infinite(blk, page);
+        }
+        if (x + 2 < end) store(buf ^ 1, x + 2);
+        __syncthreads();
+        buf ^= 1;
+    }
+
+    part = pg_uniform(kept_part); deal = pg_uniform(kept_deal);
+    // the two waves of the same rows: group 0 finishes the lower half of the fragments, group 1 the upper one
+    constexpr int HALF = NV / 2, XW = QT * (HALF * 256 + 128);
+    float* mine = lds + wv * XW;
+    const float* theirs = lds + (wv ^ 4) * XW;
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        l[qt] += __shfl_xor(l[qt], 16, 64);
+        l[qt] += __shfl_xor(l[qt], 32, 64);
+        float* to = mine + qt * (HALF * 256 + 128);
+#pragma unroll
+        for (int f = 0; f < HALF; ++f) *(f32x4_t*)(to + (f * 64 + lane) * 4) = kg == 0 ? acc[qt][HALF + f] : acc[qt][f];
+        to[HALF * 256 + lane] = R[qt];
+        to[HALF * 256 + 64 + lane] = l[qt];
+    }
+    __syncthreads();
+    const bool shared = part.len < part.blocks;
+    float* slot = a.part + (size_t)(2 * worker + (part.off == 0)) * RT * (Dh + 2);
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        const float* from = theirs + qt * (HALF * 256 + 128);
+        const float Ro = from[HALF * 256 + lane], lo = from[HALF * 256 + 64 + lane];
+        const float M = fmaxf(R[qt], Ro), wi = __builtin_amdgcn_exp2f(R[qt] - M), wo = __builtin_amdgcn_exp2f(Ro - M);
+        const float L = l[qt] * wi + lo * wo, inv = shared ? 1.f : L == 0.f ? 0.f : 1.f / L;
+        const int x = r0 + 16 * qt + lm, j = pg_token(a, x), row = first + j, h = kvh * g + x - j * g, xs = x - row0;
+        if (x >= nrows) continue;
+        const size_t at = (size_t)row * a.out_row + (size_t)h * Dh + 4 * lg;
+#pragma unroll
+        for (int f = 0; f < HALF; ++f) {
+            const f32x4_t o = ((kg == 0 ? acc[qt][f] : acc[qt][HALF + f]) * wi + *(const f32x4_t*)(from + (f * 64 + lane) * 4) * wo) * inv;
+            const int ff = kg * HALF + f;
+            if (shared) {
+                float* to = slot + xs * Dh + 16 * ff + 4 * lg;
+                st_agent_f32x2(to, o[0], o[1]);
+                st_agent_f32x2(to + 2, o[2], o[3]);
+            } else if (a.act == FASTCOT_BF16) *(uint2*)((bf16_t*)a.out + at + 16 * ff) = make_uint2(pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3]));
+            else *(f32x4_t*)((float*)a.out + at + 16 * ff) = o;
+        }
+        if (kg == 0 && lg == 0) {
+            if (shared) st_agent_f32x2(slot + RT * Dh + 2 * xs, M, L);
+            else if (a.lse) a.lse[(size_t)row * a.H + h] = M * LN2 + logf(L);
+        }
+    }
+    if (shared) {
+        const int w0 = (int)(part.base / deal.share), parts = (int)((part.base + part.blocks - 1) / deal.share) - w0 + 1;
+        wait_vmem_done();
+        __syncthreads();
+        if (tid == 0) arrived = arrive_agent(a.cnt + w0);
+        __syncthreads();
+        if (arrived == parts - 1) {
+            pg_join<G, RT, 8>(a, lds, row0, nrows, first, kvh, w0, parts);
+            if (tid == 0) st_agent_i32(a.cnt + w0, 0);
+        }
+    }
+    __syncthreads();
+  } while (pg_next<RT>(a, deal, part));
+}
+
+#define PG_WORKERS 512           // most workgroups of a launch; of those of many rows 256
+// rows of a unit of the kernel for many rows: as many tiles of a wave as find their registers
+static constexpr int many_tiles(int G, int QP) { return G > 4 ? 1 : 2; }
+// partial results: two slots a workgroup, of up to 32 rows, or of a unit of many rows
+size_t fc_paged_attn_scratch_bytes(int Dh) {
+    const size_t few = (size_t)PG_WORKERS * 2 * 32, many = (size_t)PG_WORKERS * 64 * many_tiles(Dh / 32, 1);
+    return (few > many ? few : many) * (Dh + 2) * 4;
+}
 
 template <int G, bool F32, int QT, int NW, int QP, int PP>
 static hipError_t launch_as(PagedAttnArgs a, int grid, hipStream_t st) {
@@ -521,6 +849,19 @@ static hipError_t launch_as(PagedAttnArgs a, int grid, hipStream_t st) {
 template <int G, bool F32, int QP, int PP>
 static hipError_t launch(const PagedAttnArgs& a, hipStream_t st) {
     const int cus = fc_num_cus();
+    if constexpr (!F32) {
+        if (a.r.R * a.g > 32) {
+            constexpr int QT = many_tiles(G, QP);
+            const size_t stage = 2 * 4 * 128 * G * 16, meet = 8 * QT * (G * 256 + 128) * 4, bytes = stage > meet ? stage : meet;
+            auto kernel = k_paged_many<G, QT, QP, QP>;
+            const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            if (e != hipSuccess) return e;
+            PagedAttnArgs m = a;
+            m.whole = 16;
+            kernel<<<2 * cus < PG_WORKERS ? cus : PG_WORKERS / 2, 512, bytes, st>>>(m, (a.r.R * a.g + 64 * QT - 1) / (64 * QT));
+            return hipGetLastError();
+        }
+    }
     if (a.r.R * a.g > 16) return launch_as<G, F32, 2, 4, QP, PP>(a, cus, st);
     if constexpr (G <= 4) {
         if ((int64_t)a.r.B * a.c.Hkv <= cus) return launch_as<G, F32, 1, 8, QP, PP>(a, cus, st);
