@@ -37,6 +37,7 @@ __device__ inline int pg_len(const PagedView& c, int s) {
 }
 #endif
 
+struct PagedJoin { int32_t row0, nrows, first, kvh, parts; };       // a unit whose parts a second launch joins; parts = 0: none
 struct PagedAttnArgs {
     PagedView c;
     PagedRows r;
@@ -49,7 +50,7 @@ struct PagedAttnArgs {
     int32_t esz;                           // bytes of a cached value
     int32_t window, sinks;                 // window 0: none
     int32_t whole;                         // most blocks of a unit that is not cut
-    int32_t* cnt; float* part;             // hand-off of key splits: counters (zero between launches), partial results
+    int32_t* cnt; PagedJoin* joins; float* part;       // hand-off of parts: counters (zero between launches), units to join, partial results
 };
 size_t fc_paged_attn_scratch_bytes(int Dh);
 hipError_t fc_paged_attn(const PagedAttnArgs& a, hipStream_t st);

@@ -56,17 +56,18 @@ __device__ inline void pg_far(float* p, float& by, float& from) {
 __device__ inline bool pg_sees(const PagedAttnArgs& a, int key, int pos) {
     return key <= pos && (!a.window || key > pos - a.window || key < a.sinks);
 }
-// Eight bf16 values of V: zero outside `keep`, and zero where they are not finite; whether any of those kept is not.  (An infinity or NaN is added by itself to
-// the rows that see it, whatever its weight: multiplied by a weight of zero it would reach the others.)
-__device__ inline bool pg_finite(u32x4_t& v, const uint32_t* keep) {
-    uint32_t found = 0;
+// whether any of eight bf16 values is not finite (their exponents are all ones: a carry out of each when the lowest bit is added)
+__device__ inline bool pg_not_finite(const u32x4_t& v) {
+    uint32_t x = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const uint32_t x = v[w] & keep[w], bad = ((x & 0x7F80u) == 0x7F80u ? 0x0000FFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-        v[w] = x & ~bad;
-        found |= bad;
-    }
-    return found != 0;
+    for (int w = 0; w < 4; ++w) x |= (v[w] & 0x7F807F80u) + 0x00800080u;
+    return (x & 0x80008000u) != 0;
+}
+// zeros in their place: an infinity or NaN is added by itself to the rows that see it, whatever its weight; multiplied by a weight of zero it would reach the others
+__device__ inline void pg_make_finite(u32x4_t& v) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+        v[w] &= ((v[w] & 0x7F80u) == 0x7F80u ? 0u : 0x0000FFFFu) | ((v[w] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
 }
 // What is not finite among eight values of V: ones where it is +infinity or NaN, and where it is -infinity or NaN
 __device__ inline void pg_infinite(u32x4_t& up, u32x4_t& down) {
@@ -563,7 +564,6 @@ template <int G, int QT, int QP, int PP>
 __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tiles) {
     constexpr int Dh = 32 * G, NV = 2 * G, RT = 64 * QT, SEC = 128 * G;    // SEC: 16-byte words of one block of K or V
     extern __shared__ __align__(16) float lds[];
-    __shared__ int arrived;
     __shared__ PagedPart kept_part;
     __shared__ PagedDeal kept_deal;
     __shared__ int bad[2][2];
@@ -574,6 +574,7 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
     const int per = gridDim.x >> 3, worker = gridDim.x & 7 ? blockIdx.x : (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     PagedDeal deal;
     PagedPart part;
+    if (tid == 0) a.joins[worker].parts = 0;
     if (!pg_deal<RT>(a, tiles, worker, gridDim.x, deal, part)) return;
     const float scale2 = LOG2E / sqrtf((float)Dh);
     const float unscaled = QP == 1 ? scale2 : 1.f;             // what turns a product into an exponent of two
@@ -651,13 +652,12 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
             u32x4_t v = stage[i];
             if (sec & 1) {
                 const int y = x + (sec >> 1), kb = (y < vis.sunk ? y : y - vis.sunk + vis.lo) << 5;
-                uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
                 if (kb + 31 > plast) {
                     const int past = kb + 8 * lg;              // the positions of this lane's eight values
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) keep[w] = (past + 2 * w <= plast ? 0x0000FFFFu : 0u) | (past + 2 * w + 1 <= plast ? 0xFFFF0000u : 0u);
+                    for (int w = 0; w < 4; ++w) v[w] &= (past + 2 * w <= plast ? 0x0000FFFFu : 0u) | (past + 2 * w + 1 <= plast ? 0xFFFF0000u : 0u);
                 }
-                if (pg_finite(v, keep)) bad[buf][sec >> 1] = x;
+                if (pg_not_finite(v)) { pg_make_finite(v); bad[buf][sec >> 1] = x; }
             }
             kv[buf * 4 * SEC + i * 512 + tid] = v;
         }
@@ -795,30 +795,62 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
             const f32x4_t o = ((kg == 0 ? acc[qt][f] : acc[qt][HALF + f]) * wi + *(const f32x4_t*)(from + (f * 64 + lane) * 4) * wo) * inv;
             const int ff = kg * HALF + f;
             if (shared) {
-                float* to = slot + xs * Dh + 16 * ff + 4 * lg;
-                st_agent_f32x2(to, o[0], o[1]);
-                st_agent_f32x2(to + 2, o[2], o[3]);
+                *(f32x4_t*)(slot + xs * Dh + 16 * ff + 4 * lg) = o;
             } else if (a.act == FASTCOT_BF16) *(uint2*)((bf16_t*)a.out + at + 16 * ff) = make_uint2(pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3]));
             else *(f32x4_t*)((float*)a.out + at + 16 * ff) = o;
         }
         if (kg == 0 && lg == 0) {
-            if (shared) st_agent_f32x2(slot + RT * Dh + 2 * xs, M, L);
+            if (shared) *(float2*)(slot + RT * Dh + 2 * xs) = make_float2(M, L);
             else if (a.lse) a.lse[(size_t)row * a.H + h] = M * LN2 + logf(L);
         }
     }
-    if (shared) {
-        const int w0 = (int)(part.base / deal.share), parts = (int)((part.base + part.blocks - 1) / deal.share) - w0 + 1;
-        wait_vmem_done();
-        __syncthreads();
-        if (tid == 0) arrived = arrive_agent(a.cnt + w0);
-        __syncthreads();
-        if (arrived == parts - 1) {
-            pg_join<G, RT, 8>(a, lds, row0, nrows, first, kvh, w0, parts);
-            if (tid == 0) st_agent_i32(a.cnt + w0, 0);
-        }
+    if (shared && part.off == 0 && tid == 0) {
+        const int w0 = (int)(part.base / deal.share);          // (this worker)
+        a.joins[w0] = PagedJoin{row0, nrows, first, kvh, (int)((part.base + part.blocks - 1) / deal.share) - w0 + 1};
     }
     __syncthreads();
   } while (pg_next<RT>(a, deal, part));
+}
+
+// Joins the units that several workgroups of k_paged_many share, 16 rows a workgroup (a launch of its own: the last workgroup to arrive would read
+// 66 KB a part alone, 60 us for 16 rows of 64 heads on 8 over 2000 positions)
+template <int G, int RT>
+__global__ __launch_bounds__(256, 1) void k_paged_join(PagedAttnArgs a) {
+    constexpr int Dh = 32 * G, SLOT = RT * (Dh + 2);
+    const int w0 = blockIdx.x / (RT / 16), chunk = blockIdx.x % (RT / 16);
+    const PagedJoin j = a.joins[w0];
+    const float* p0 = a.part + (size_t)(2 * w0 + 1) * SLOT;    // the first part's slot; the others' are the even ones behind it
+    for (int y = threadIdx.x; y < 16 * Dh / 4; y += 256) {
+        const int r = 16 * chunk + y / (Dh / 4), d = 4 * (y % (Dh / 4));
+        if (j.parts == 0 || j.row0 + r >= j.nrows) return;
+        float M = -INFINITY, L = 0.f;
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        for (int i0 = 0; i0 < j.parts; i0 += 8) {
+            float2 ml[8];
+            f32x4_t v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = i0 + e < j.parts ? i0 + e : i0;
+                const float* s = p0 + (i ? (size_t)(2 * i - 1) * SLOT : 0);
+                ml[e] = *(const float2*)(s + RT * Dh + 2 * r);
+                v[e] = *(const f32x4_t*)(s + r * Dh + d);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (i0 + e >= j.parts) continue;
+                const float Mn = fmaxf(M, ml[e].x), x = __builtin_amdgcn_exp2f(M - Mn), w = __builtin_amdgcn_exp2f(ml[e].x - Mn);
+                L = L * x + ml[e].y * w;
+                o = o * x + v[e] * w;
+                M = Mn;
+            }
+        }
+        const int tk = pg_token(a, j.row0 + r), row = j.first + tk, h = j.kvh * a.g + j.row0 + r - tk * a.g;
+        o *= L == 0.f ? 0.f : 1.f / L;
+        const size_t at = (size_t)row * a.out_row + (size_t)h * Dh + d;
+        if (a.act == FASTCOT_BF16) *(uint2*)((bf16_t*)a.out + at) = make_uint2(pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3]));
+        else *(f32x4_t*)((float*)a.out + at) = o;
+        if (a.lse && d == 0) a.lse[(size_t)row * a.H + h] = M * LN2 + logf(L);
+    }
 }
 
 #define PG_WORKERS 512           // most workgroups of a launch; of those of many rows 256
@@ -858,7 +890,9 @@ static hipError_t launch(const PagedAttnArgs& a, hipStream_t st) {
             if (e != hipSuccess) return e;
             PagedAttnArgs m = a;
             m.whole = 16;
-            kernel<<<2 * cus < PG_WORKERS ? cus : PG_WORKERS / 2, 512, bytes, st>>>(m, (a.r.R * a.g + 64 * QT - 1) / (64 * QT));
+            const int grid = cus < PG_WORKERS / 2 ? cus : PG_WORKERS / 2;
+            kernel<<<grid, 512, bytes, st>>>(m, (a.r.R * a.g + 64 * QT - 1) / (64 * QT));
+            k_paged_join<G, 64 * QT><<<grid * 4 * QT, 256, 0, st>>>(m);
             return hipGetLastError();
         }
     }
