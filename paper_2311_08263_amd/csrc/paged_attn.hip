@@ -566,7 +566,7 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
     extern __shared__ __align__(16) float lds[];
     __shared__ PagedPart kept_part;
     __shared__ PagedDeal kept_deal;
-    __shared__ int bad[2][2];
+    __shared__ int bad[2][2], redo;
     u32x4_t* kv = (u32x4_t*)lds;                               // [buffer][block of the pair][K, V][SEC]
     const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv >> 2, rg = wv & 3;
@@ -612,12 +612,6 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
     f32x4_t acc[QT][NV];
     float R[QT], l[QT];                                        // reference of the row's exponents, this lane's share of the sum of weights
     bool far = false;                                          // some reference is far from zero
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        R[qt] = ROW_NONE; l[qt] = 0.f;
-#pragma unroll
-        for (int f = 0; f < NV; ++f) acc[qt][f] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    }
 
     // pages of 64 blocks of the part at a time, one a lane: those at hand and the next ones (-1: no page, the block is not used)
     auto pages_from = [&](int x0) {
@@ -625,9 +619,10 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
         const int page = seq >= 0 && x < end && slot < a.c.MP ? table[slot] : -1;
         return page >= 0 && page < a.c.N ? page : -1;
     };
-    int now = pages_from(part.off), next = pages_from(part.off + 64), held = part.off;         // held: the first block of those at hand
+    int now, next, held;                                       // held: the first block of those at hand
     const int inpage = (1 << a.c.pb) - 1;
     u32x4_t stage[G];
+    const uint32_t lane16 = lane * 16;
     // requests the pair of blocks x, x + 1, whose pages become page0 and page1
     int page0, page1;
     auto load = [&](int x) {
@@ -640,11 +635,13 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
 #pragma unroll
         for (int i = 0; i < G; ++i) {
             const int w0 = i * 512 + wv * 64, sec = G == 4 ? i : w0 / SEC;         // sec: block of the pair, K or V
-            stage[i] = *((const u32x4_t*)(sec & 1 ? a.vl : a.kl) + (sec & 2 ? at1 : at0) + (w0 - sec * SEC) + lane);
+            const char* from = (sec & 1 ? a.vl : a.kl) + ((sec & 2 ? at1 : at0) + (w0 - sec * SEC)) * 16;
+            stage[i] = *(const u32x4_t*)(pg_uniform(from) + lane16);
         }
     };
-    // puts the pair of blocks x, x + 1 into a buffer.  V goes in with zeros for what is not finite, and where the unit's last row does not see it: a weight of zero
-    // times an infinity would be none.  Of what is not finite and seen `bad` keeps the pair's number; it is added by itself to the rows that see it
+    // puts the pair of blocks x, x + 1 into a buffer.  V gets zeros where the unit's last row does not see it (a weight of zero times an infinity would be none) and,
+    // in a careful walk, for what is not finite: of that `bad` keeps the pair's number, and it is added by itself to the rows that see it
+    bool careful = false;
     auto store = [&](int buf, int x) {
 #pragma unroll
         for (int i = 0; i < G; ++i) {
@@ -657,7 +654,7 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
 #pragma unroll
                     for (int w = 0; w < 4; ++w) v[w] &= (past + 2 * w <= plast ? 0x0000FFFFu : 0u) | (past + 2 * w + 1 <= plast ? 0xFFFF0000u : 0u);
                 }
-                if (pg_not_finite(v)) { pg_make_finite(v); bad[buf][sec >> 1] = x; }
+                if (careful && pg_not_finite(v)) { pg_make_finite(v); bad[buf][sec >> 1] = x; }
             }
             kv[buf * 4 * SEC + i * 512 + tid] = v;
         }
@@ -739,28 +736,50 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
         }
     };
 
-    if (tid < 4) bad[tid >> 1][tid & 1] = -1;
-    if (tid == 0) { kept_part = part; kept_deal = deal; }      // (scalar registers are short in the walk)
-    load(part.off);
-    __syncthreads();
-    store(0, part.off);
-    __syncthreads();
-    int buf = 0;
-    for (int x = part.off; x < end; x += 2) {
-        const int blk = x + kg < vis.sunk ? x + kg : x + kg - vis.sunk + vis.lo, kb = blk << 5, page = kg ? page1 : page0;
-        if (x + 2 < end) load(x + 2);                          // travels while this pair is used
-        __builtin_amdgcn_sched_barrier(0);
-        // does any row of the wave see the block, and do all of them see all of it
-        const bool seen = any_rows && page >= 0 && kb <= p1 && (!a.window || kb + 31 > p0 - a.window || kb < a.sinks);
-        const bool whole = kb + 31 <= p0 && (!a.window || kb > p1 - a.window || kb + 31 < a.sinks);
-        if (seen) {
-            const u32x4_t* at = kv + (buf * 4 + 2 * kg) * SEC;
-            compute(at, kb, whole);
-            if (bad[buf][kg] == x) add_infinite(blk, page);
+    if (tid == 0) { kept_part = part; kept_deal = deal; redo = 0; }        // (scalar registers are short in the walk)
+    for (;;) {
+        now = pages_from(part.off); next = pages_from(part.off + 64); held = part.off;
+        far = false;
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            R[qt] = ROW_NONE; l[qt] = 0.f;
+#pragma unroll
+            for (int f = 0; f < NV; ++f) acc[qt][f] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
         }
-        if (x + 2 < end) store(buf ^ 1, x + 2);
+        if (tid < 4) bad[tid >> 1][tid & 1] = -1;
+        load(part.off);
         __syncthreads();
-        buf ^= 1;
+        store(0, part.off);
+        __syncthreads();
+        int buf = 0;
+        for (int x = part.off; x < end; x += 2) {
+            const int blk = x + kg < vis.sunk ? x + kg : x + kg - vis.sunk + vis.lo, kb = blk << 5, page = kg ? page1 : page0;
+            if (x + 2 < end) load(x + 2);                          // travels while this pair is used
+            __builtin_amdgcn_sched_barrier(0);
+            // does any row of the wave see the block, and do all of them see all of it
+            const bool seen = any_rows && page >= 0 && kb <= p1 && (!a.window || kb + 31 > p0 - a.window || kb < a.sinks);
+            const bool whole = kb + 31 <= p0 && (!a.window || kb > p1 - a.window || kb + 31 < a.sinks);
+            if (seen) {
+                const u32x4_t* at = kv + (buf * 4 + 2 * kg) * SEC;
+                compute(at, kb, whole);
+                if (careful && bad[buf][kg] == x) add_infinite(blk, page);
+            }
+            if (x + 2 < end) store(buf ^ 1, x + 2);
+            __syncthreads();
+            buf ^= 1;
+        }
+        if (careful) break;
+        float z = 0.f;                                         // not a number where a sum is not finite
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+            for (int f = 0; f < NV; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z = fmaf(acc[qt][f][i], 0.f, z);
+        if (z != z) redo = 1;
+        __syncthreads();
+        if (!redo) break;
+        careful = true;                                        // once more: V is not finite somewhere (or a query or a key is not)
     }
 
     part = pg_uniform(kept_part); deal = pg_uniform(kept_deal);
