@@ -553,6 +553,11 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
   } while (pg_next<RT>(a, deal, part));
 }
 
+// The kernel for many rows: tiles of a wave, groups of rows (a wave for the even and one for the odd blocks each), and whether the lower parts of
+// fp32 queries lie in LDS: what finds its registers without spilling, and 160 KB.
+static constexpr int many_tiles(int G) { return G > 4 ? 1 : 2; }
+static constexpr int many_groups(int G, int QP) { return G == 8 && QP == 3 ? 2 : 4; }
+static constexpr bool many_low(int G, int QP) { return G < 8 && QP == 3; }
 // Many rows of a sequence (prompt chunks, wide windows, windows over grouped heads; bf16 caches): 64 * QT rows a unit.  Four waves of 16 * QT rows take the even
 // blocks, four with the same rows the odd ones; a pair of blocks goes global -> LDS while the previous pair is used, so that K and V are
 // read once for all the unit's rows and a fragment from LDS once for a wave's QT tiles.  At the end the two waves of the same rows exchange half of their sums.
@@ -560,16 +565,18 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
 // exponentials for bf16 rows.  To keep those few, sums are taken relative to a reference that moves only when a score passes it by 8 powers of two (so
 // weights are at most 2^8, and nothing is rescaled in most blocks).  With bf16 rows the weights are rounded to bf16 once in front of the product
 // with V: as large an error as the rounding of the output, half a step of each weight; their sum is taken before the rounding.
-template <int G, int QT, int QP, int PP>
-__global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tiles) {
-    constexpr int Dh = 32 * G, NV = 2 * G, RT = 64 * QT, SEC = 128 * G;    // SEC: 16-byte words of one block of K or V
+template <int G, int QT, int RG, int QP, int PP>
+__global__ __launch_bounds__(128 * RG, 1) void k_paged_many(PagedAttnArgs a, int tiles) {
+    constexpr int Dh = 32 * G, NV = 2 * G, RT = 16 * RG * QT, SEC = 128 * G, T = 128 * RG;        // SEC: 16-byte words of one block of K or V
     extern __shared__ __align__(16) float lds[];
     __shared__ PagedPart kept_part;
     __shared__ PagedDeal kept_deal;
     __shared__ int bad[2][2], redo;
+    constexpr bool LOW = many_low(G, QP);
+    u32x4_t* ql = (u32x4_t*)lds + 8 * SEC;                     // LOW: the lower parts of fp32 queries [row group][tile][fragment][part][64]
     u32x4_t* kv = (u32x4_t*)lds;                               // [buffer][block of the pair][K, V][SEC]
     const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lg = lane >> 4;
-    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv >> 2, rg = wv & 3;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv / RG, rg = wv % RG;
     // consecutive shares on one XCD: units of one K/V head follow each other and find its blocks in that L2
     const int per = gridDim.x >> 3, worker = gridDim.x & 7 ? blockIdx.x : (blockIdx.x & 7) * per + (blockIdx.x >> 3);
     PagedDeal deal;
@@ -592,7 +599,7 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
     const int end = part.off + part.len;
 
     int pos[QT];
-    u32x4_t qf[QT][G][QP];
+    u32x4_t qf[QT][G][LOW ? 1 : QP];                           // queries, or their upper parts
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int x = r0 + 16 * qt + lm, row = x < nrows ? x : nrows - 1, j = pg_token(a, row);
@@ -605,7 +612,11 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
             else {
                 const float4 y = *(const float4*)((const float*)a.q + at + dh), z = *(const float4*)((const float*)a.q + at + dh + 4);
                 const float v[8] = {y.x * scale2, y.y * scale2, y.z * scale2, y.w * scale2, z.x * scale2, z.y * scale2, z.z * scale2, z.w * scale2};
-                pg_split8<QP>(v, qf[qt][f]);
+                u32x4_t parts[QP];
+                pg_split8<QP>(v, parts);
+#pragma unroll
+                for (int q = 0; q < (LOW ? 1 : QP); ++q) qf[qt][f][q] = parts[q];
+                if constexpr (LOW) ql[(((rg * QT + qt) * G + f) * 2 + kg) * 64 + lane] = kg ? parts[2] : parts[1];
             }
         }
     }
@@ -621,7 +632,7 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
     };
     int now, next, held;                                       // held: the first block of those at hand
     const int inpage = (1 << a.c.pb) - 1;
-    u32x4_t stage[G];
+    u32x4_t stage[4 * G / RG];
     const uint32_t lane16 = lane * 16;
     // requests the pair of blocks x, x + 1, whose pages become page0 and page1
     int page0, page1;
@@ -633,8 +644,8 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
         const size_t at0 = ((((size_t)(page0 < 0 ? 0 : page0) * a.c.Hkv + kvh) << a.c.pb) + (b0 & inpage)) * SEC;
         const size_t at1 = ((((size_t)(page1 < 0 ? 0 : page1) * a.c.Hkv + kvh) << a.c.pb) + (b1 & inpage)) * SEC;
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-            const int w0 = i * 512 + wv * 64, sec = G == 4 ? i : w0 / SEC;         // sec: block of the pair, K or V
+        for (int i = 0; i < 4 * G / RG; ++i) {
+            const int w0 = i * T + wv * 64, sec = SEC % T ? w0 / SEC : i * T / SEC;         // sec: block of the pair, K or V
             const char* from = (sec & 1 ? a.vl : a.kl) + ((sec & 2 ? at1 : at0) + (w0 - sec * SEC)) * 16;
             stage[i] = *(const u32x4_t*)(pg_uniform(from) + lane16);
         }
@@ -644,8 +655,8 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
     bool careful = false;
     auto store = [&](int buf, int x) {
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-            const int w0 = i * 512 + wv * 64, sec = G == 4 ? i : w0 / SEC;
+        for (int i = 0; i < 4 * G / RG; ++i) {
+            const int w0 = i * T + wv * 64, sec = SEC % T ? w0 / SEC : i * T / SEC;
             u32x4_t v = stage[i];
             if (sec & 1) {
                 const int y = x + (sec >> 1), kb = (y < vis.sunk ? y : y - vis.sunk + vis.lo) << 5;
@@ -656,7 +667,7 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
                 }
                 if (careful && pg_not_finite(v)) { pg_make_finite(v); bad[buf][sec >> 1] = x; }
             }
-            kv[buf * 4 * SEC + i * 512 + tid] = v;
+            kv[buf * 4 * SEC + i * T + tid] = v;
         }
     };
 
@@ -670,55 +681,83 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
 #pragma unroll
         for (int f = 0; f < 2 * G; ++f) kf[f] = kb_lds[f * 64 + lane];
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);                         // (the other wave of the SIMD has exponentials to do)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int f = 0; f < G; ++f) {
+            if constexpr (QP == 3) {                           // (small parts first)
+                u32x4_t lower[2][QT];
 #pragma unroll
-            for (int f = 0; f < G; ++f) {
-                const bf16x8_t k = __builtin_bit_cast(bf16x8_t, kf[t * G + f]);
+                for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-                for (int q = QP - 1; q >= 0; --q)
+                    for (int q = 1; q >= 0; --q) lower[q][qt] = LOW ? ql[(((rg * QT + qt) * G + f) * 2 + q) * 64 + lane] : qf[qt][f][LOW ? 0 : q + 1];
 #pragma unroll
-                    for (int qt = 0; qt < QT; ++qt) sc[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8_t, qf[qt][f][q]), sc[qt][t], 0, 0, 0);
+                for (int q = 1; q >= 0; --q)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int qt = 0; qt < QT; ++qt)
+                            sc[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[t * G + f]), __builtin_bit_cast(bf16x8_t, lower[q][qt]), sc[qt][t], 0, 0, 0);
             }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt)
+                    sc[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[t * G + f]), __builtin_bit_cast(bf16x8_t, qf[qt][f][0]), sc[qt][t], 0, 0, 0);
+        }
 #pragma unroll
         for (int f = 0; f < NV; ++f) vf[f] = vb_lds[f * 64 + lane];
-        __builtin_amdgcn_sched_barrier(0);
-        u32x4_t pf[QT][PP];
+        __builtin_amdgcn_s_setprio(0);
+        float p[QT][8], by = unscaled, from[QT], top[QT];
+        bool moves = false;                                    // weights are 2^(by * p - from)
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[qt][e] = sc[qt][e >> 2][e & 3];
+        if (!whole) {
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[qt][e] = pg_sees(a, kb + 8 * lg + e, pos[qt]) ? p[qt][e] : -INFINITY;
+        }
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
-            float p[8], top = -INFINITY;
+            top[qt] = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = sc[qt][e >> 2][e & 3];
-            if (!whole) {
+            for (int e = 0; e < 8; ++e) top[qt] = fmaxf(top[qt], p[qt][e]);
+            top[qt] *= by;
+            moves |= top[qt] > R[qt] + 8.f;
+        }
+        if (__any(moves)) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = pg_sees(a, kb + 8 * lg + e, pos[qt]) ? p[e] : -INFINITY;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, p[e]);
-            float by = unscaled, from = R[qt];                 // weights are 2^(by * p - from)
-            if (__any(by * top > from + 8.f)) {
-                top *= by;
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float Rn = fmaxf(R[qt], top), alpha = __builtin_amdgcn_exp2f(R[qt] - Rn);
-                R[qt] = from = Rn;
-                far = far || __any(Rn > 1048576.f || (Rn < -1048576.f && Rn > ROW_NONE));
+            for (int qt = 0; qt < QT; ++qt) {
+                float m = fmaxf(top[qt], __shfl_xor(top[qt], 16, 64));
+                m = fmaxf(m, __shfl_xor(m, 32, 64));
+                if (!(m > R[qt] + 8.f)) m = R[qt];
+                const float alpha = __builtin_amdgcn_exp2f(R[qt] - m);
+                R[qt] = m;
+                far = far || __any(m > 1048576.f || (m < -1048576.f && m > ROW_NONE));
                 l[qt] *= alpha;
 #pragma unroll
                 for (int f = 0; f < NV; ++f) acc[qt][f] *= alpha;
             }
-            if (QP == 1 && far) pg_far(p, by, from);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], by, -from)); l[qt] += p[e]; }
-            pg_split8<PP>(p, pf[qt]);
         }
 #pragma unroll
-        for (int f = 0; f < NV; ++f) {
-            const bf16x8_t v = __builtin_bit_cast(bf16x8_t, vf[f]);
+        for (int qt = 0; qt < QT; ++qt) from[qt] = R[qt];
+        if (QP == 1 && far) {
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) { by = unscaled; pg_far(p[qt], by, from[qt]); }
+        }
+        // one tile's weights beside another one's products
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            u32x4_t pf[PP];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { p[qt][e] = __builtin_amdgcn_exp2f(fmaf(p[qt][e], by, -from[qt])); l[qt] += p[qt][e]; }
+            pg_split8<PP>(p[qt], pf);
 #pragma unroll
             for (int q = PP - 1; q >= 0; --q)
 #pragma unroll
-                for (int qt = 0; qt < QT; ++qt) acc[qt][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, pf[qt][q]), acc[qt][f], 0, 0, 0);
+                for (int f = 0; f < NV; ++f) acc[qt][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf[f]), __builtin_bit_cast(bf16x8_t, pf[q]), acc[qt][f], 0, 0, 0);
         }
     };
     // what is not finite in V of block blk of a page, for the rows that see it
@@ -786,7 +825,7 @@ __global__ __launch_bounds__(512, 1) void k_paged_many(PagedAttnArgs a, int tile
     // the two waves of the same rows: group 0 finishes the lower half of the fragments, group 1 the upper one
     constexpr int HALF = NV / 2, XW = QT * (HALF * 256 + 128);
     float* mine = lds + wv * XW;
-    const float* theirs = lds + (wv ^ 4) * XW;
+    const float* theirs = lds + (wv ^ RG) * XW;
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         l[qt] += __shfl_xor(l[qt], 16, 64);
@@ -873,11 +912,9 @@ __global__ __launch_bounds__(256, 1) void k_paged_join(PagedAttnArgs a) {
 }
 
 #define PG_WORKERS 512           // most workgroups of a launch; of those of many rows 256
-// rows of a unit of the kernel for many rows: as many tiles of a wave as find their registers
-static constexpr int many_tiles(int G, int QP) { return G > 4 ? 1 : 2; }
 // partial results: two slots a workgroup, of up to 32 rows, or of a unit of many rows
 size_t fc_paged_attn_scratch_bytes(int Dh) {
-    const size_t few = (size_t)PG_WORKERS * 2 * 32, many = (size_t)PG_WORKERS * 64 * many_tiles(Dh / 32, 1);
+    const size_t few = (size_t)PG_WORKERS * 2 * 32, many = (size_t)PG_WORKERS * 64 * many_tiles(Dh / 32);
     return (few > many ? few : many) * (Dh + 2) * 4;
 }
 
@@ -902,16 +939,17 @@ static hipError_t launch(const PagedAttnArgs& a, hipStream_t st) {
     const int cus = fc_num_cus();
     if constexpr (!F32) {
         if (a.r.R * a.g > 32) {
-            constexpr int QT = many_tiles(G, QP);
-            const size_t stage = 2 * 4 * 128 * G * 16, meet = 8 * QT * (G * 256 + 128) * 4, bytes = stage > meet ? stage : meet;
-            auto kernel = k_paged_many<G, QT, QP, QP>;
+            constexpr int QT = many_tiles(G), RG = many_groups(G, QP), RT = 16 * RG * QT;
+            const size_t stage = 2 * 4 * 128 * G * 16, low = many_low(G, QP) ? RG * QT * G * 2 * 1024 : 0, meet = 2 * RG * QT * (G * 256 + 128) * 4;
+            const size_t bytes = stage + low > meet ? stage + low : meet;
+            auto kernel = k_paged_many<G, QT, RG, QP, QP>;
             const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
             if (e != hipSuccess) return e;
             PagedAttnArgs m = a;
             m.whole = 16;
             const int grid = cus < PG_WORKERS / 2 ? cus : PG_WORKERS / 2;
-            kernel<<<grid, 512, bytes, st>>>(m, (a.r.R * a.g + 64 * QT - 1) / (64 * QT));
-            k_paged_join<G, 64 * QT><<<grid * 4 * QT, 256, 0, st>>>(m);
+            kernel<<<grid, 128 * RG, bytes, st>>>(m, (a.r.R * a.g + RT - 1) / RT);
+            k_paged_join<G, RT><<<grid * (RT / 16), 256, 0, st>>>(m);
             return hipGetLastError();
         }
     }
