@@ -112,7 +112,7 @@ struct PagedPart {
     int off, len, blocks;
     uint32_t base;                         // place of the unit's first block in what is dealt
 };
-struct PagedDeal { uint32_t share, at, end; };         // what a workgroup gets, and this one's places: at .. end - 1
+struct PagedDeal { uint32_t share, at, end; int least; };         // what a workgroup gets, this one's places at .. end - 1, fewest blocks of a part
 __device__ inline int pg_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // a structure of 32-bit words that is the same in every lane
 template <class T> __device__ inline T pg_uniform(const T& x) {
@@ -156,14 +156,22 @@ __device__ inline uint32_t pg_lane(uint32_t v, int l) { return (uint32_t)__built
 // tiles).  A unit of at most a.whole blocks is not cut, it belongs to the share that its first block falls into.  The host has checked that all
 // places fit 31 bits.  false: nothing for this worker.  p: the first part of its share.
 // A unit's queries, meeting and output take about as long as eight blocks: 48 sequences of 60 to 8100 positions over 40 heads take 302 us with 4 places a
-// unit, 256 with 8, 255 with 16; three short ones 10.9, 8.7 and 8.7 us, 200 of 20 to 300 positions over 8 heads 32.8, 32.9 and 35.3.
-#define PG_UNIT 8
+// unit, 256 with 8, 255 with 16; three short ones 10.9, 8.7 and 8.7 us, 200 of 20 to 300 positions over 8 heads 32.8, 32.9 and 35.3.  (The kernel for many
+// rows: 4.3 us a unit, 0.72 us a block.)
+#define PG_UNIT (RT > 32 ? 6 : 8)
 template <int RT> __device__ inline void pg_part(const PagedAttnArgs& a, PagedDeal& d, PagedPart& p) {     // the share's part of the unit p, from the place d.at on
     if (p.blocks <= a.whole) { p.off = 0; p.len = p.base >= d.at && p.base < d.end ? p.blocks : 0; return; }
-    p.off = d.at > p.base ? (int)(d.at - p.base) : 0;
-    const int left = d.end > p.base ? (int)(d.end - p.base) : 0;           // places of the unit's blocks in front of the share's end
-    p.len = (left < p.blocks ? left : p.blocks) - p.off;
+    // (a cut close to an end of the unit is moved there)
+    auto cut = [&](uint32_t place) {
+        const int c = (int)(place - p.base);
+        return c < d.least ? 0 : p.blocks - c < d.least ? p.blocks : c;
+    };
+    p.off = cut(d.at);
+    p.len = cut(d.end) - p.off;
 }
+// workgroups that share a cut unit
+__device__ inline int pg_first_worker(const PagedDeal& d, const PagedPart& p) { return (int)((p.base + d.least - 1) / d.share); }
+__device__ inline int pg_last_worker(const PagedDeal& d, const PagedPart& p) { return (int)((p.base + p.blocks - d.least) / d.share); }
 template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int tiles, int worker, int workers, PagedDeal& d, PagedPart& p) {
     const int lane = threadIdx.x & 63, Hkv = a.c.Hkv;
     const bool by_seq = tiles <= 4;
@@ -185,6 +193,7 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
     }
     d.share = (total + workers - 1) / workers;
     if (d.share < PG_UNIT) d.share = PG_UNIT;
+    d.least = d.share < 32 ? 1 : d.share < 64 ? 2 : 4;
     d.at = d.share * worker;
     if (d.at >= total) return false;
     d.end = d.at + d.share < total ? d.at + d.share : total;
@@ -541,7 +550,7 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
     if (shared) {
         wait_vmem_done();
         __syncthreads();
-        const int w0 = (int)(part.base / deal.share), parts = (int)((part.base + part.blocks - 1) / deal.share) - w0 + 1;
+        const int w0 = pg_first_worker(deal, part), parts = pg_last_worker(deal, part) - w0 + 1;
         if (threadIdx.x == 0) arrived = arrive_agent(a.cnt + w0);
         __syncthreads();
         if (arrived == parts - 1) {
@@ -863,8 +872,7 @@ __global__ __launch_bounds__(128 * RG, 1) void k_paged_many(PagedAttnArgs a, int
         }
     }
     if (shared && part.off == 0 && tid == 0) {
-        const int w0 = (int)(part.base / deal.share);          // (this worker)
-        a.joins[w0] = PagedJoin{row0, nrows, first, kvh, (int)((part.base + part.blocks - 1) / deal.share) - w0 + 1};
+        a.joins[worker] = PagedJoin{row0, nrows, first, kvh, pg_last_worker(deal, part) - worker + 1};
     }
     __syncthreads();
   } while (pg_next<RT>(a, deal, part));
