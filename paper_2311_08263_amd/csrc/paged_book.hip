@@ -285,48 +285,69 @@ __global__ __launch_bounds__(256) void k_paged_reset(PagedView c) {
     for (size_t i = i0; i < (size_t)c.N; i += step) c.ref[i] = 0;
 }
 
-// eight values of a row in the cache's type
-__device__ inline void pg_load8(const void* p, size_t at, int act, float* v) {
-    if (act == FASTCOT_BF16) {
-        const uint4 u = *(const uint4*)((const bf16_t*)p + at);
+template <typename A> __device__ inline float pg_value(A x) { if constexpr (sizeof(A) == 2) return bf16_to_f32(x); else return x; }
+// eight values next to each other
+template <typename A> __device__ inline void pg_load8(const A* p, float* v) {
+    if constexpr (sizeof(A) == 2) {
+        const uint4 u = *(const uint4*)p;
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(w[e] << 16); v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
     } else {
-        const float4 x = *(const float4*)((const float*)p + at), y = *(const float4*)((const float*)p + at + 4);
+        const float4 x = *(const float4*)p, y = *(const float4*)(p + 4);
         v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
     }
 }
+template <typename T> __device__ inline void pg_store8(T* p, const float* v) {
+    if constexpr (sizeof(T) == 2) *(uint4*)p = make_uint4(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7]));
+    else { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]); }
+}
 
-// grid: x over a sequence's rows x heads x eights of a head, y over sequences
-template <int DT>
-__global__ __launch_bounds__(256) void k_paged_write(PagedView c, PagedRows r, int Dh, char* kl, char* vl, const void* k, const void* v, int64_t row_stride, int act) {
-    typedef typename std::conditional<DT == FASTCOT_BF16, bf16_t, float>::type T;
-    const int i = blockIdx.y, D8 = Dh >> 3, s = pg_seq(r, c, i);
+// New rows into the pages, a workgroup per block of 32 positions and K/V head (grid: x over blocks and heads, y over sequences).  Threads go by what they store,
+// whole 16-byte pieces in the order of the block (V: eight positions of a head element; pieces that the rows fill in part, value by value), so stores are
+// whole lines and what a line of the rows is read for twice comes out of the L1.  Bound by HBM, one token of each sequence by latency.  (A thread per eight
+// elements of a row, V stored value by value: 4096 fp32 rows of 32 heads 143 us.)
+template <typename T, typename A>
+__global__ __launch_bounds__(256) void k_paged_write(PagedView c, PagedRows r, T* kl, T* vl, const A* k, const A* v, int64_t row_stride) {
+    const int i = blockIdx.y, s = pg_seq(r, c, i), G = c.Dh >> 5, tid = threadIdx.x;
+    if (s < 0) return;
     int first, count;
     pg_rows(r, i, first, count);
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int d8 = (int)(x % D8), h = (int)(x / D8 % c.Hkv), j = (int)(x / D8 / c.Hkv);
-    if (s < 0 || j >= count) return;
-    const int64_t pos = (int64_t)pg_len(c, s) + j;
-    const int64_t slot = pos >> (c.pb + 5);
-    if (slot >= c.MP) return;
+    const int n = pg_len(c, s), h = blockIdx.x % c.Hkv, blk = (n >> 5) + blockIdx.x / c.Hkv, p0 = blk << 5;
+    const int slot = blk >> c.pb;
+    if (p0 >= n + count || slot >= c.MP) return;
     const int page = c.table[(size_t)s * c.MP + slot];
     if (pg_none(c, page)) return;
-    float a[8], b[8];
-    const size_t at = (size_t)(first + j) * row_stride + (size_t)h * Dh + 8 * d8;
-    pg_load8(k, at, act, a);
-    pg_load8(v, at, act, b);
-    const int p = (int)(pos & ((32 << c.pb) - 1));
-    const size_t base = (((size_t)page * c.Hkv + h) << c.pb) * 32 * Dh;
-    T* kd = (T*)kl + base; T* vd = (T*)vl + base;
-    if constexpr (DT == FASTCOT_BF16) {
-        *(uint4*)(kd + k_index(p, 8 * d8, Dh)) = make_uint4(pk_bf16(a[0], a[1]), pk_bf16(a[2], a[3]), pk_bf16(a[4], a[5]), pk_bf16(a[6], a[7]));
+    const size_t base = ((((size_t)page * c.Hkv + h) << c.pb) + (blk & ((1 << c.pb) - 1))) * 32 * c.Dh;
+    const A* kr = k + (int64_t)(first + p0 - n) * row_stride + (size_t)h * c.Dh;       // the row of position p0 (which may lie in front of the first one)
+    const A* vr = v + (int64_t)(first + p0 - n) * row_stride + (size_t)h * c.Dh;
+    const int lo = n - p0 > 0 ? n - p0 : 0, hi = n + count - p0 < 32 ? n + count - p0 : 32;          // positions of the block that are written
+    for (int x = tid; x < 32 * G; x += 256) {                  // a position and 32 elements: one piece of four fragments each
+        const int t = x / (16 * G), y = x % (16 * G), q = y & 15, p = 8 * (q >> 2) + 4 * t + (q & 3);
+        if (p < lo || p >= hi) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vd[v_index(8 * d8 + e, p, Dh)] = (bf16_t)(pk_bf16(b[e], 0.f) & 0xFFFF);
-    } else {
+        for (int f = 0; f < 4; ++f) {
+            float a[8];
+            pg_load8(kr + p * row_stride + 32 * (y >> 4) + 8 * f, a);
+            pg_store8(kl + base + (size_t)((t * 4 + f) * 16 * G + y) * 8, a);
+        }
+    }
+    for (int x = tid; x < 4 * c.Dh; x += 256) {
+        const int d = (x >> 6) * 16 + (x & 15), p = 8 * (x >> 4 & 3);
+        T* to = vl + base + (size_t)x * 8;
+        float a[8];
+        if (p >= lo && p + 8 <= hi) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { kd[k_index(p, 8 * d8 + e, Dh)] = a[e]; vd[v_index(8 * d8 + e, p, Dh)] = b[e]; }
+            for (int e = 0; e < 8; ++e) a[e] = pg_value(vr[(p + e) * row_stride + d]);
+            pg_store8(to, a);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (p + e < lo || p + e >= hi) continue;
+                const float y = pg_value(vr[(p + e) * row_stride + d]);
+                if constexpr (sizeof(T) == 2) to[e] = (T)(pk_bf16(y, 0.f) & 0xFFFF); else to[e] = y;
+            }
+        }
     }
 }
 
@@ -473,12 +494,14 @@ extern "C" int fastcot_paged_write(const fastcot_paged* c, int32_t layer, const 
     if (row_stride % 8 || row_stride < (int64_t)c->n_kv_heads * c->head_dim) FAIL(FASTCOT_EINVAL, "%s: row stride below a row or no multiple of 8", name);
     char* kl = v.k + (size_t)layer * c->n_pages * page_bytes(c);
     char* vl = v.v + (size_t)layer * c->n_pages * page_bytes(c);
-    const int64_t per = (int64_t)r.R * c->n_kv_heads * (c->head_dim / 8), gx = (per + 255) / 256;
+    const int64_t gx = ((int64_t)(r.R + 31) / 32 + 1) * c->n_kv_heads;             // (rows may begin inside a block)
     if (gx > 0x7FFFFFFF) FAIL(FASTCOT_ECAPACITY, "%s: too many rows of one sequence", name);
     const dim3 grid((unsigned)gx, (unsigned)r.B);
     hipStream_t st = (hipStream_t)hip_stream;
-    if (c->dtype == FASTCOT_BF16) k_paged_write<FASTCOT_BF16><<<grid, 256, 0, st>>>(v, r, c->head_dim, kl, vl, d_k, d_v, row_stride, act_dtype);
-    else k_paged_write<FASTCOT_F32><<<grid, 256, 0, st>>>(v, r, c->head_dim, kl, vl, d_k, d_v, row_stride, act_dtype);
+    if (c->dtype == FASTCOT_F32) k_paged_write<float, float><<<grid, 256, 0, st>>>(v, r, (float*)kl, (float*)vl, (const float*)d_k, (const float*)d_v, row_stride);
+    else if (act_dtype == FASTCOT_F32)
+        k_paged_write<bf16_t, float><<<grid, 256, 0, st>>>(v, r, (bf16_t*)kl, (bf16_t*)vl, (const float*)d_k, (const float*)d_v, row_stride);
+    else k_paged_write<bf16_t, bf16_t><<<grid, 256, 0, st>>>(v, r, (bf16_t*)kl, (bf16_t*)vl, (const bf16_t*)d_k, (const bf16_t*)d_v, row_stride);
     return launched(name, hipGetLastError());
 }
 extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const fastcot_paged_rows* rows, const void* d_q, int64_t q_row_stride,
