@@ -256,10 +256,15 @@ __global__ __launch_bounds__(PG_WG) void k_paged_compact(PagedView c, int32_t* d
     if (threadIdx.x == 0) { *n_moves = moves; if (d_used) *d_used = used; }
 }
 
-// Copies page data by a list of moves, block by block; blocks == NULL: whole pages.  With a map the table follows.
+// Copies page data by a list of moves, block by block: of a fork the first blocks[m] of each page, the copies of one block after each other (children of one
+// sequence read it from the L2 then), of a compaction whole pages, and the table follows the map.  What is written goes past the caches, and what a
+// compaction reads, once, too (15 children of a 7B sequence 274 us with everything cached, 308 with nothing, 189 so; 1.1 GB compacted 453, 426 so, of
+// which 4.9 TB/s, the rate of a large copy, are 458).
+template <bool FORK>
 __global__ __launch_bounds__(256) void k_paged_move(PagedView c, int block16, const int* n_moves, const int* from, const int* to, const int* blocks, const int* map) {
+    typedef __attribute__((__vector_size__(16))) uint32_t u32x4;
     const int moves = *n_moves, tid = threadIdx.x;
-    if (map)
+    if (!FORK)
         for (size_t i = (size_t)blockIdx.x * 256 + tid; i < (size_t)c.S * c.MP; i += (size_t)gridDim.x * 256) {
             const int page = c.table[i];
             if (!pg_none(c, page)) c.table[i] = map[page];
@@ -267,14 +272,14 @@ __global__ __launch_bounds__(256) void k_paged_move(PagedView c, int block16, co
     const int PB = 1 << c.pb;
     const int64_t per = (int64_t)c.L * 2 * c.Hkv << c.pb, all = per * moves;
     for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
-        const int m = (int)(x / per);
-        const uint32_t y = (uint32_t)(x - m * per), blk = y & (PB - 1), z = y >> c.pb, h = z % c.Hkv, w = z / c.Hkv;
-        if (blocks && (int)blk >= blocks[m]) continue;
+        const int m = FORK ? (int)(x % moves) : (int)(x / per);
+        const uint32_t y = FORK ? (uint32_t)(x / moves) : (uint32_t)(x - m * per), blk = y & (PB - 1), z = y >> c.pb, h = z % c.Hkv, w = z / c.Hkv;
+        if (FORK && (int)blk >= blocks[m]) continue;
         char* pool = w & 1 ? c.v : c.k;
         const size_t layer = (size_t)(w >> 1) * c.N;
-        const uint4* a = (const uint4*)pool + ((((layer + from[m]) * c.Hkv + h) << c.pb) + blk) * block16;
-        uint4* b = (uint4*)pool + ((((layer + to[m]) * c.Hkv + h) << c.pb) + blk) * block16;
-        for (int e = tid; e < block16; e += 256) b[e] = a[e];
+        const u32x4* a = (const u32x4*)pool + ((((layer + from[m]) * c.Hkv + h) << c.pb) + blk) * block16;
+        u32x4* b = (u32x4*)pool + ((((layer + to[m]) * c.Hkv + h) << c.pb) + blk) * block16;
+        for (int e = tid; e < block16; e += 256) __builtin_nontemporal_store(FORK ? a[e] : __builtin_nontemporal_load(a + e), b + e);
     }
 }
 
@@ -447,7 +452,7 @@ extern "C" int fastcot_paged_fork(const fastcot_paged* c, int32_t count, const i
     hipStream_t st = (hipStream_t)hip_stream;
     k_paged_fork<<<1, PG_WG, 0, st>>>(v, count, d_src, d_dst, d_status, n, from, to, blocks);
     TRY(launched(name, hipGetLastError()));
-    k_paged_move<<<8 * fc_num_cus(), 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, blocks, nullptr);
+    k_paged_move<true><<<32 * fc_num_cus(), 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, blocks, nullptr);
     return launched(name, hipGetLastError());
 }
 extern "C" int fastcot_paged_trim(const fastcot_paged* c, int32_t count, const int32_t* d_seqs, int32_t window, int32_t sinks, int32_t* d_status, void* hip_stream) {
@@ -479,7 +484,7 @@ extern "C" int fastcot_paged_compact(const fastcot_paged* c, int32_t* d_used, vo
     hipStream_t st = (hipStream_t)hip_stream;
     k_paged_compact<<<1, PG_WG, 0, st>>>(v, d_used, n, from, to, map);
     TRY(launched(name, hipGetLastError()));
-    k_paged_move<<<8 * fc_num_cus(), 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, nullptr, map);
+    k_paged_move<false><<<32 * fc_num_cus(), 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, nullptr, map);
     return launched(name, hipGetLastError());
 }
 extern "C" int fastcot_paged_write(const fastcot_paged* c, int32_t layer, const fastcot_paged_rows* rows, const void* d_k, const void* d_v, int64_t row_stride,
