@@ -493,10 +493,10 @@ class PagedCache:
         dev = torch.device(device if device is not None else given[0].device if given else "cuda")
         self.device = torch.device("cuda", torch.cuda.current_device() if dev.index is None else dev.index)
         self.dtype = dtype
+        self._index = self.device.index
         self._desc = PagedDesc(n_layers, n_pages, page_size, n_kv_heads, head_dim, 1 if dtype == torch.bfloat16 else 0, max_seqs, max_pages)
-        self._ref = ctypes.byref(self._desc)
-        L = lib()
-        nbytes, sbytes = L.fastcot_paged_pool_bytes(self._ref), L.fastcot_paged_scratch_bytes(self._ref)
+        self._lib = L = lib()
+        nbytes, sbytes = L.fastcot_paged_pool_bytes(self._desc), L.fastcot_paged_scratch_bytes(self._desc)
         if nbytes == 0:
             raise _bad("invalid cache description")
         shape = (n_layers, n_pages, n_kv_heads, page_size // 32, 32 * head_dim)
@@ -513,57 +513,66 @@ class PagedCache:
         self.len = self.book[max_seqs * max_pages:max_seqs * (max_pages + 1)]
         self.ref = self.book[max_seqs * (max_pages + 1):]
         self.scratch = torch.zeros(sbytes, dtype=torch.uint8, device=self.device)
+        self._scratch = self.scratch.data_ptr()
         d = self._desc
         d.k_pool, d.v_pool = self.k.data_ptr(), self.v.data_ptr()
         d.table, d.len, d.ref = self.table.data_ptr(), self.len.data_ptr(), self.ref.data_ptr()
         if book is None:
-            self._call(L.fastcot_paged_reset, self._ref)
+            self._call(L.fastcot_paged_reset, self._desc)
         torch.cuda.synchronize(self.device)          # whatever stream the calls run on, they find it made
 
     def _call(self, fn, *args) -> None:
-        torch, dev = _gpu_torch, self.device.index
-        if torch.cuda.current_device() == dev:
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+        C, dev = _gpu_torch._C, self._index
+        if C._cuda_getDevice() == dev:
+            rc = fn(*args, C._cuda_getCurrentRawStream(dev))
         else:
-            with torch.cuda.device(dev):
-                rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
-        _check(rc)
+            with _gpu_torch.cuda.device(dev):
+                rc = fn(*args, C._cuda_getCurrentRawStream(dev))
+        if rc:
+            _check(rc)
 
     def _ints(self, t, what: str, n: Optional[int] = None):
-        if t.dtype != _gpu_torch.int32 or t.device != self.device or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        if t.dtype is not _gpu_torch.int32 or t.get_device() != self._index or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
             raise _bad(f"{what}: a contiguous int32 tensor{'' if n is None else f' of {n}'} on {self.device}")
         return t.data_ptr()
 
-    def _entries(self, fn, a, b, *more):
-        status = _gpu_torch.empty(a.numel(), dtype=_gpu_torch.int32, device=self.device)
-        args = (self._ints(a, "sequences"),) + (() if b is None else (self._ints(b, "the second argument", a.numel()),))
-        self._call(fn, self._ref, a.numel(), *args, *more[:-1], status.data_ptr(), *more[-1])
-        return status
-
     def grow(self, seqs, rows):
         """Pages for the next rows[i] positions of each sequence."""
-        return self._entries(lib().fastcot_paged_grow, seqs, rows, (self.scratch.data_ptr(),))
+        n, s = seqs.numel(), self._ints(seqs, "seqs")
+        r, status = self._ints(rows, "rows", n), _gpu_torch.empty_like(seqs)
+        self._call(self._lib.fastcot_paged_grow, self._desc, n, s, r, status.data_ptr(), self._scratch)
+        return status
 
     def advance(self, seqs, rows):
         """len += rows[i]: the rows are committed."""
-        return self._entries(lib().fastcot_paged_advance, seqs, rows, ())
+        n, s = seqs.numel(), self._ints(seqs, "seqs")
+        r, status = self._ints(rows, "rows", n), _gpu_torch.empty_like(seqs)
+        self._call(self._lib.fastcot_paged_advance, self._desc, n, s, r, status.data_ptr())
+        return status
 
     def fork(self, src, dst):
         """The empty sequence dst[i] continues src[i]."""
-        return self._entries(lib().fastcot_paged_fork, src, dst, (self.scratch.data_ptr(),))
+        n, s = src.numel(), self._ints(src, "src")
+        d, status = self._ints(dst, "dst", n), _gpu_torch.empty_like(src)
+        self._call(self._lib.fastcot_paged_fork, self._desc, n, s, d, status.data_ptr(), self._scratch)
+        return status
 
     def trim(self, seqs, window: int, sinks: int = 0):
         """Pages that a sliding window has left behind leave the sequences."""
-        return self._entries(lib().fastcot_paged_trim, seqs, None, window, sinks, ())
+        s, status = self._ints(seqs, "seqs"), _gpu_torch.empty_like(seqs)
+        self._call(self._lib.fastcot_paged_trim, self._desc, seqs.numel(), s, window, sinks, status.data_ptr())
+        return status
 
     def free(self, seqs):
         """The sequences end."""
-        return self._entries(lib().fastcot_paged_free, seqs, None, ())
+        s, status = self._ints(seqs, "seqs"), _gpu_torch.empty_like(seqs)
+        self._call(self._lib.fastcot_paged_free, self._desc, seqs.numel(), s, status.data_ptr())
+        return status
 
     def compact(self):
         """Pages in use move to the front of the pools; returns their number (a device int32)."""
         used = _gpu_torch.empty((), dtype=_gpu_torch.int32, device=self.device)
-        self._call(lib().fastcot_paged_compact, self._ref, used.data_ptr(), self.scratch.data_ptr())
+        self._call(self._lib.fastcot_paged_compact, self._desc, used.data_ptr(), self._scratch)
         return used
 
     def _rows(self, n_rows: int, seqs, row_start, max_rows: Optional[int]) -> PagedRows:
@@ -575,49 +584,46 @@ class PagedCache:
             return PagedRows(n_seqs, n_rows // max(n_seqs, 1), n_rows, ps, None)
         return PagedRows(n_seqs, n_rows if max_rows is None else max_rows, n_rows, ps, self._ints(row_start, "row_start", n_seqs + 1))
 
-    def _act(self, t, shape, what: str) -> int:
-        torch = _gpu_torch
-        if t.device != self.device or tuple(t.shape[1:]) != shape or t.dim() != 3 or t.dtype not in (torch.float32, torch.bfloat16) or \
+    def _act(self, t, heads: int, what: str) -> int:
+        torch, dt = _gpu_torch, t.dtype
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self._desc.head_dim or t.get_device() != self._index or (dt is not torch.float32 and dt is not torch.bfloat16) or \
                 (t.stride(2) != 1 and t.numel()):
-            raise _bad(f"{what}: fp32 or bf16 rows x {shape} on {self.device}, head elements next to each other")
-        return 0 if t.dtype == torch.float32 else 1
+            raise _bad(f"{what}: fp32 or bf16 rows x {heads} x {self._desc.head_dim} on {self.device}, head elements next to each other")
+        return 0 if dt is torch.float32 else 1
 
     def write(self, k, v, layer: int = 0, seqs=None, row_start=None, max_rows: Optional[int] = None) -> None:
         """k, v [rows, n_kv_heads, head_dim] of the sequences' next positions into a layer.  Without row_start every sequence has as many rows;
         with it (int32 on the device, one more entry than sequences) sequence i has rows row_start[i] .. row_start[i + 1] - 1, at most max_rows."""
-        d = self._desc
-        shape = (d.n_kv_heads, d.head_dim)
-        act = self._act(k, shape, "k")
-        if self._act(v, shape, "v") != act or v.shape != k.shape:
+        Hkv, Dh = self._desc.n_kv_heads, self._desc.head_dim
+        act, n, row = self._act(k, Hkv, "k"), k.shape[0], Hkv * Dh
+        if self._act(v, Hkv, "v") != act or v.shape[0] != n:
             raise _bad("k and v differ in type or rows")
-        n, row = k.shape[0], d.n_kv_heads * d.head_dim
-        if d.n_kv_heads > 1 and n and (k.stride(1) != d.head_dim or v.stride(1) != d.head_dim):
+        if n and Hkv > 1 and (k.stride(1) != Dh or v.stride(1) != Dh):
             raise _bad("the heads of a row of k and v follow each other")
         if n > 1:
             row = k.stride(0)
             if v.stride(0) != row:
                 raise _bad("the rows of k and v are at different strides")
-        r = self._rows(n, seqs, row_start, max_rows)
-        self._call(lib().fastcot_paged_write, self._ref, layer, ctypes.byref(r), k.data_ptr(), v.data_ptr(), row, act)
+        self._call(self._lib.fastcot_paged_write, self._desc, layer, self._rows(n, seqs, row_start, max_rows), k.data_ptr(), v.data_ptr(), row, act)
 
     def attn(self, q, layer: int = 0, seqs=None, row_start=None, max_rows: Optional[int] = None, window: int = 0, sinks: int = 0, out=None,
              want_lse: bool = False, scratch=None):
         """q [rows, heads, head_dim] (rows as for write, already written) -> out [rows, heads * head_dim] of q's type, and with want_lse the log of
         the sum of exp(score), fp32 [rows, heads].  Calls that may overlap in time need a scratch of their own (zeros like self.scratch)."""
-        torch, d = _gpu_torch, self._desc
+        torch, Dh = _gpu_torch, self._desc.head_dim
         n, H = q.shape[0], q.shape[1] if q.dim() == 3 else 0
-        act = self._act(q, (H, d.head_dim), "q")
+        act, cols = self._act(q, H, "q"), H * Dh
         if out is None:
-            out = torch.empty(n, H * d.head_dim, dtype=q.dtype, device=self.device)
-        elif out.dtype != q.dtype or out.device != self.device or tuple(out.shape) != (n, H * d.head_dim) or (out.stride(1) != 1 and n):
-            raise _bad(f"out: {q.dtype} {(n, H * d.head_dim)} on {self.device}")
+            out = q.new_empty((n, cols))
+        elif out.dtype is not q.dtype or out.get_device() != self._index or tuple(out.shape) != (n, cols) or (out.stride(1) != 1 and n):
+            raise _bad(f"out: {q.dtype} {(n, cols)} on {self.device}")
         lse = torch.empty(n, H, dtype=torch.float32, device=self.device) if want_lse else None
-        if scratch is None:
-            scratch = self.scratch
-        elif scratch.device != self.device or not scratch.is_contiguous() or scratch.numel() * scratch.element_size() < self.scratch.numel():
-            raise _bad(f"scratch: {self.scratch.numel()} zeroed bytes on {self.device}")
-        r = self._rows(n, seqs, row_start, max_rows)
-        self._call(lib().fastcot_paged_attn, self._ref, layer, ctypes.byref(r), q.data_ptr(), q.stride(0) if n > 1 else H * d.head_dim,
-                   q.stride(1) if H > 1 else d.head_dim, H, act, window, sinks, out.data_ptr(), out.stride(0) if n > 1 else H * d.head_dim,
-                   lse.data_ptr() if want_lse else None, scratch.data_ptr())
+        at = self._scratch
+        if scratch is not None:
+            if scratch.get_device() != self._index or not scratch.is_contiguous() or scratch.numel() * scratch.element_size() < self.scratch.numel():
+                raise _bad(f"scratch: {self.scratch.numel()} zeroed bytes on {self.device}")
+            at = scratch.data_ptr()
+        self._call(self._lib.fastcot_paged_attn, self._desc, layer, self._rows(n, seqs, row_start, max_rows), q.data_ptr(), q.stride(0) if n > 1 else cols,
+                   q.stride(1) if H > 1 else Dh, H, act, window, sinks, out.data_ptr(), out.stride(0) if n > 1 else cols,
+                   lse.data_ptr() if want_lse else None, at)
         return (out, lse) if want_lse else out

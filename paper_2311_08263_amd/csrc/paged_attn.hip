@@ -176,9 +176,9 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
     const int lane = threadIdx.x & 63, Hkv = a.c.Hkv;
     const bool by_seq = tiles <= 4;
     // places of one K/V head of sequence b in tiles t0 .. t1 - 1
+    int seq = -1, n = 0, first = 0, rows = 0;                  // of the sequence that was looked at last
     auto places = [&](int b, int t0, int t1) -> uint32_t {
         if (b >= a.r.B) return 0;
-        int seq, n, first, rows;
         pg_load(a, b, seq, n, first, rows);
         uint32_t s = 0;
         for (int t = t0; t < t1; ++t) { const int x = pg_blocks<RT>(a, seq, n, rows, t); s += x ? x + PG_UNIT : 0; }
@@ -199,7 +199,7 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
     d.end = d.at + d.share < total ? d.at + d.share : total;
     // the sequence that place d.at falls into, the places in front of it, and those of one of its heads
     uint32_t before = 0, head = 0;
-    int b = 0;
+    int b = 0, from = 0;                                       // from: a lane that has looked at it
     if (by_seq) {
         for (;; b += 64) {
             if (a.r.B > 64) { mine = places(b + lane, 0, tiles) * Hkv; incl = pg_wave_scan(mine); }
@@ -210,6 +210,7 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
                 before += pg_lane(incl, l) - w;
                 head = w / Hkv;
                 b += l;
+                from = l;
                 break;
             }
             before += pg_lane(incl, 63);
@@ -224,8 +225,8 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
         }
     }
     p.b = b;
-    pg_load(a, b, p.seq, p.n, p.first, p.rows);
-    p.seq = pg_uniform(p.seq); p.n = pg_uniform(p.n); p.first = pg_uniform(p.first); p.rows = pg_uniform(p.rows);
+    p.seq = __builtin_amdgcn_readlane(seq, from); p.n = __builtin_amdgcn_readlane(n, from);
+    p.first = __builtin_amdgcn_readlane(first, from); p.rows = __builtin_amdgcn_readlane(rows, from);
     p.kvh = pg_uniform((int)((d.at - before) / head));
     before += head * p.kvh;
     p.tile = 0;
@@ -388,11 +389,19 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
         for (int f = 0; f < NV; ++f) acc[qt][f] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int x = part.off + wv; x < part.off + part.len; x += NW) {
+    // pages of this wave's next 64 blocks, one a lane
+    const int end = part.off + part.len;
+    auto pages_from = [&](int x0) {
+        const int x = x0 + lane * NW, blk = x < vis.sunk ? x : x - vis.sunk + vis.lo, slot = blk >> a.c.pb;
+        const int page = seq >= 0 && x < end && slot < a.c.MP ? table[slot] : -1;
+        return page >= 0 && page < a.c.N ? page : -1;
+    };
+    int pages = pages_from(part.off + wv), held = part.off + wv;
+    for (int x = held; x < end; x += NW) {
+        if (x - held == 64 * NW) { held = x; pages = pages_from(x); }
         const int blk = x < vis.sunk ? x : x - vis.sunk + vis.lo, kb = blk << 5;
-        const int slot = blk >> a.c.pb;
-        const int page = slot < a.c.MP && seq >= 0 ? table[slot] : -1;
-        if (page < 0 || page >= a.c.N) continue;
+        const int page = __builtin_amdgcn_readlane(pages, (x - held) / NW);
+        if (page < 0) continue;
         const size_t at = ((((size_t)page * a.c.Hkv + kvh) << a.c.pb) + (blk & ((1 << a.c.pb) - 1))) * 32 * Dh;
         constexpr int FW = F32 ? 2 : 1;                        // 16-byte words of a lane's eight values
         const u32x4_t* kp = (const u32x4_t*)(a.kl + at * (F32 ? 4 : 2)) + lane * FW;

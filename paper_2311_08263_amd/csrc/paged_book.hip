@@ -364,7 +364,7 @@ static bool shape_ok(const fastcot_paged* c) {
     return c && c->n_layers >= 1 && c->n_layers <= 4096 && c->n_pages >= 1 && c->n_pages <= PG_MAX_PAGES && c->page_size >= 32 && c->page_size <= 4096 &&
            !(c->page_size & (c->page_size - 1)) && c->n_kv_heads >= 1 && c->n_kv_heads <= 4096 && head_dim_ok(c->head_dim) &&
            (c->dtype == FASTCOT_F32 || c->dtype == FASTCOT_BF16) && c->max_seqs >= 1 && c->max_seqs <= PG_MAX_SEQS && c->max_pages >= 1 &&
-           (int64_t)c->max_pages * c->page_size <= (int64_t)1 << 30;
+           (int64_t)c->max_pages * c->page_size <= (int64_t)1 << 30 && (int64_t)c->n_layers * c->n_kv_heads * (c->page_size / 16) < (int64_t)1 << 31;
 }
 static size_t esz_of(const fastcot_paged* c) { return c->dtype == FASTCOT_BF16 ? 2 : 4; }
 static size_t page_bytes(const fastcot_paged* c) { return (size_t)c->n_kv_heads * c->page_size * c->head_dim * esz_of(c); }
@@ -452,7 +452,9 @@ extern "C" int fastcot_paged_fork(const fastcot_paged* c, int32_t count, const i
     hipStream_t st = (hipStream_t)hip_stream;
     k_paged_fork<<<1, PG_WG, 0, st>>>(v, count, d_src, d_dst, d_status, n, from, to, blocks);
     TRY(launched(name, hipGetLastError()));
-    k_paged_move<true><<<32 * fc_num_cus(), 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, blocks, nullptr);
+    const int64_t most = (int64_t)count * c->n_layers * c->n_kv_heads * (c->page_size / 16);         // (blocks that can be copied)
+    const int grid = most < 32 * fc_num_cus() ? (int)most : 32 * fc_num_cus();
+    k_paged_move<true><<<grid, 256, 0, st>>>(v, (int)(32 * c->head_dim * esz_of(c) / 16), n, from, to, blocks, nullptr);
     return launched(name, hipGetLastError());
 }
 extern "C" int fastcot_paged_trim(const fastcot_paged* c, int32_t count, const int32_t* d_seqs, int32_t window, int32_t sinks, int32_t* d_status, void* hip_stream) {
