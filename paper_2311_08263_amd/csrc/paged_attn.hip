@@ -335,7 +335,7 @@ template <int G, int RT, int NW> __device__ inline void pg_join(const PagedAttnA
 
 // G: 32s of a head; F32: fp32 cache; QT: tiles of 16 rows of a unit; NW: waves; QP, PP: bf16 parts of queries and weights
 template <int G, bool F32, int QT, int NW, int QP, int PP>
-__global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int tiles) {
+__global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_attn(PagedAttnArgs a, int tiles) {
     constexpr int Dh = 32 * G, NV = 2 * G, RT = 16 * QT;       // NV: fragments of V, four sums of a lane each
     constexpr int PART = Dh * 16 + 32;                         // floats of a wave's tile: sums, then m and l of the 16 rows
     extern __shared__ __align__(16) float lds[];
@@ -571,10 +571,11 @@ __global__ __launch_bounds__(NW * 64, 1) void k_paged_attn(PagedAttnArgs a, int 
   } while (pg_next<RT>(a, deal, part));
 }
 
-// The kernel for many rows: tiles of a wave, groups of rows (a wave for the even and one for the odd blocks each), and whether the lower parts of
-// fp32 queries lie in LDS: what finds its registers without spilling, and 160 KB.
+// The kernel for many rows: tiles of a wave, groups of rows (KG waves each), waves on a SIMD, and whether the lower
+// parts of fp32 queries lie in LDS: what finds its registers without spilling, and 160 KB.
 static constexpr int many_tiles(int G) { return G > 4 ? 1 : 2; }
 static constexpr int many_groups(int G, int QP) { return G == 8 && QP == 3 ? 2 : 4; }
+static constexpr int many_waves(int G, int QP) { return G == 8 && QP == 3 ? 1 : 2; }
 static constexpr bool many_low(int G, int QP) { return G < 8 && QP == 3; }
 // Many rows of a sequence (prompt chunks, wide windows, windows over grouped heads; bf16 caches): 64 * QT rows a unit.  Four waves of 16 * QT rows take the even
 // blocks, four with the same rows the odd ones; a pair of blocks goes global -> LDS while the previous pair is used, so that K and V are
@@ -583,16 +584,16 @@ static constexpr bool many_low(int G, int QP) { return G < 8 && QP == 3; }
 // exponentials for bf16 rows.  To keep those few, sums are taken relative to a reference that moves only when a score passes it by 8 powers of two (so
 // weights are at most 2^8, and nothing is rescaled in most blocks).  With bf16 rows the weights are rounded to bf16 once in front of the product
 // with V: as large an error as the rounding of the output, half a step of each weight; their sum is taken before the rounding.
-template <int G, int QT, int RG, int QP, int PP>
-__global__ __launch_bounds__(128 * RG, 1) void k_paged_many(PagedAttnArgs a, int tiles) {
-    constexpr int Dh = 32 * G, NV = 2 * G, RT = 16 * RG * QT, SEC = 128 * G, T = 128 * RG;        // SEC: 16-byte words of one block of K or V
+template <int G, int QT, int RG, int KG, int QP, int PP>
+__global__ __launch_bounds__(64 * RG * KG, many_waves(G, QP)) void k_paged_many(PagedAttnArgs a, int tiles) {
+    constexpr int Dh = 32 * G, NV = 2 * G, RT = 16 * RG * QT, SEC = 128 * G, T = 64 * RG * KG;    // SEC: 16-byte words of one block of K or V
     extern __shared__ __align__(16) float lds[];
     __shared__ PagedPart kept_part;
     __shared__ PagedDeal kept_deal;
-    __shared__ int bad[2][2], redo;
+    __shared__ int bad[2][KG], redo;
     constexpr bool LOW = many_low(G, QP);
-    u32x4_t* ql = (u32x4_t*)lds + 8 * SEC;                     // LOW: the lower parts of fp32 queries [row group][tile][fragment][part][64]
-    u32x4_t* kv = (u32x4_t*)lds;                               // [buffer][block of the pair][K, V][SEC]
+    u32x4_t* ql = (u32x4_t*)lds + 4 * KG * SEC;                     // LOW: the lower parts of fp32 queries [row group][tile][fragment][part][64]
+    u32x4_t* kv = (u32x4_t*)lds;                               // [buffer][block of the stage][K, V][SEC]
     const int tid = threadIdx.x, lane = tid & 63, lm = lane & 15, lg = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv / RG, rg = wv % RG;
     // consecutive shares on one XCD: units of one K/V head follow each other and find its blocks in that L2
@@ -652,24 +653,26 @@ __global__ __launch_bounds__(128 * RG, 1) void k_paged_many(PagedAttnArgs a, int
     const int inpage = (1 << a.c.pb) - 1;
     u32x4_t stage[4 * G / RG];
     const uint32_t lane16 = lane * 16;
-    // requests the pair of blocks x, x + 1, whose pages become page0 and page1
-    int page0, page1;
+    // requests blocks x .. x + KG - 1, whose pages become page[]
+    int page[KG];
     auto load = [&](int x) {
         if (x - held == 64) { held += 64; now = next; next = pages_from(held + 64); }
-        page0 = __builtin_amdgcn_readlane(now, x - held);
-        page1 = __builtin_amdgcn_readlane(now, x + 1 - held);
-        const int b0 = x < vis.sunk ? x : x - vis.sunk + vis.lo, b1 = x + 1 < vis.sunk ? x + 1 : x + 1 - vis.sunk + vis.lo;
-        const size_t at0 = ((((size_t)(page0 < 0 ? 0 : page0) * a.c.Hkv + kvh) << a.c.pb) + (b0 & inpage)) * SEC;
-        const size_t at1 = ((((size_t)(page1 < 0 ? 0 : page1) * a.c.Hkv + kvh) << a.c.pb) + (b1 & inpage)) * SEC;
+        size_t at[KG];
+#pragma unroll
+        for (int y = 0; y < KG; ++y) {
+            page[y] = __builtin_amdgcn_readlane(now, x + y - held);
+            const int blk = x + y < vis.sunk ? x + y : x + y - vis.sunk + vis.lo;
+            at[y] = ((((size_t)(page[y] < 0 ? 0 : page[y]) * a.c.Hkv + kvh) << a.c.pb) + (blk & inpage)) * SEC;
+        }
 #pragma unroll
         for (int i = 0; i < 4 * G / RG; ++i) {
-            const int w0 = i * T + wv * 64, sec = SEC % T ? w0 / SEC : i * T / SEC;         // sec: block of the pair, K or V
-            const char* from = (sec & 1 ? a.vl : a.kl) + ((sec & 2 ? at1 : at0) + (w0 - sec * SEC)) * 16;
+            const int w0 = i * T + wv * 64, sec = SEC % T ? w0 / SEC : i * T / SEC;         // sec: block of the stage, K or V
+            const char* from = (sec & 1 ? a.vl : a.kl) + ((sec & 2 ? at[KG - 1] : at[0]) + (w0 - sec * SEC)) * 16;
             stage[i] = *(const u32x4_t*)(pg_uniform(from) + lane16);
         }
     };
-    // puts the pair of blocks x, x + 1 into a buffer.  V gets zeros where the unit's last row does not see it (a weight of zero times an infinity would be none) and,
-    // in a careful walk, for what is not finite: of that `bad` keeps the pair's number, and it is added by itself to the rows that see it
+    // puts blocks x .. x + KG - 1 into a buffer.  V gets zeros where the unit's last row does not see it (a weight of zero times an infinity would be none) and,
+    // in a careful walk, for what is not finite: of that `bad` keeps the stage's first block, and it is added by itself to the rows that see it
     bool careful = false;
     auto store = [&](int buf, int x) {
 #pragma unroll
@@ -685,7 +688,7 @@ __global__ __launch_bounds__(128 * RG, 1) void k_paged_many(PagedAttnArgs a, int
                 }
                 if (careful && pg_not_finite(v)) { pg_make_finite(v); bad[buf][sec >> 1] = x; }
             }
-            kv[buf * 4 * SEC + i * T + tid] = v;
+            kv[buf * 2 * KG * SEC + i * T + tid] = v;
         }
     };
 
@@ -803,25 +806,25 @@ __global__ __launch_bounds__(128 * RG, 1) void k_paged_many(PagedAttnArgs a, int
 #pragma unroll
             for (int f = 0; f < NV; ++f) acc[qt][f] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
         }
-        if (tid < 4) bad[tid >> 1][tid & 1] = -1;
+        if (tid < 2 * KG) bad[tid / KG][tid % KG] = -1;
         load(part.off);
         __syncthreads();
         store(0, part.off);
         __syncthreads();
         int buf = 0;
-        for (int x = part.off; x < end; x += 2) {
-            const int blk = x + kg < vis.sunk ? x + kg : x + kg - vis.sunk + vis.lo, kb = blk << 5, page = kg ? page1 : page0;
-            if (x + 2 < end) load(x + 2);                          // travels while this pair is used
+        for (int x = part.off; x < end; x += KG) {
+            const int blk = x + kg < vis.sunk ? x + kg : x + kg - vis.sunk + vis.lo, kb = blk << 5, here = page[kg ? KG - 1 : 0];
+            if (x + KG < end) load(x + KG);                        // travels while this stage is used
             __builtin_amdgcn_sched_barrier(0);
             // does any row of the wave see the block, and do all of them see all of it
-            const bool seen = any_rows && page >= 0 && kb <= p1 && (!a.window || kb + 31 > p0 - a.window || kb < a.sinks);
+            const bool seen = any_rows && x + kg < end && here >= 0 && kb <= p1 && (!a.window || kb + 31 > p0 - a.window || kb < a.sinks);
             const bool whole = kb + 31 <= p0 && (!a.window || kb > p1 - a.window || kb + 31 < a.sinks);
             if (seen) {
-                const u32x4_t* at = kv + (buf * 4 + 2 * kg) * SEC;
+                const u32x4_t* at = kv + (buf * 2 * KG + 2 * kg) * SEC;
                 compute(at, kb, whole);
-                if (careful && bad[buf][kg] == x) add_infinite(blk, page);
+                if (careful && bad[buf][kg] == x) add_infinite(blk, here);
             }
-            if (x + 2 < end) store(buf ^ 1, x + 2);
+            if (x + KG < end) store(buf ^ 1, x + KG);
             __syncthreads();
             buf ^= 1;
         }
@@ -840,36 +843,43 @@ __global__ __launch_bounds__(128 * RG, 1) void k_paged_many(PagedAttnArgs a, int
     }
 
     part = pg_uniform(kept_part); deal = pg_uniform(kept_deal);
-    // the two waves of the same rows: group 0 finishes the lower half of the fragments, group 1 the upper one
-    constexpr int HALF = NV / 2, XW = QT * (HALF * 256 + 128);
-    float* mine = lds + wv * XW;
+    // two waves of the same rows exchange half of their sums: group 0 finishes the lower half of the fragments, group 1 the upper one
+    constexpr int FW = NV / KG, XW = QT * (FW * 256 + 128);
     const float* theirs = lds + (wv ^ RG) * XW;
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         l[qt] += __shfl_xor(l[qt], 16, 64);
         l[qt] += __shfl_xor(l[qt], 32, 64);
-        float* to = mine + qt * (HALF * 256 + 128);
+        if constexpr (KG == 2) {
+            float* to = lds + wv * XW + qt * (FW * 256 + 128);
 #pragma unroll
-        for (int f = 0; f < HALF; ++f) *(f32x4_t*)(to + (f * 64 + lane) * 4) = kg == 0 ? acc[qt][HALF + f] : acc[qt][f];
-        to[HALF * 256 + lane] = R[qt];
-        to[HALF * 256 + 64 + lane] = l[qt];
+            for (int f = 0; f < FW; ++f) *(f32x4_t*)(to + (f * 64 + lane) * 4) = kg == 0 ? acc[qt][NV - FW + f] : acc[qt][f];
+            to[FW * 256 + lane] = R[qt];
+            to[FW * 256 + 64 + lane] = l[qt];
+        }
     }
-    __syncthreads();
+    if constexpr (KG == 2) __syncthreads();
     const bool shared = part.len < part.blocks;
     float* slot = a.part + (size_t)(2 * worker + (part.off == 0)) * RT * (Dh + 2);
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        const float* from = theirs + qt * (HALF * 256 + 128);
-        const float Ro = from[HALF * 256 + lane], lo = from[HALF * 256 + 64 + lane];
-        const float M = fmaxf(R[qt], Ro), wi = __builtin_amdgcn_exp2f(R[qt] - M), wo = __builtin_amdgcn_exp2f(Ro - M);
-        const float L = l[qt] * wi + lo * wo, inv = shared ? 1.f : L == 0.f ? 0.f : 1.f / L;
+        const float* from = theirs + qt * (FW * 256 + 128);
+        float M = R[qt], L = l[qt], wi = 1.f, wo = 0.f;
+        if constexpr (KG == 2) {
+            const float Ro = from[FW * 256 + lane];
+            M = fmaxf(R[qt], Ro); wi = __builtin_amdgcn_exp2f(R[qt] - M); wo = __builtin_amdgcn_exp2f(Ro - M);
+            L = l[qt] * wi + from[FW * 256 + 64 + lane] * wo;
+        }
+        const float inv = shared ? 1.f : L == 0.f ? 0.f : 1.f / L;
         const int x = r0 + 16 * qt + lm, j = pg_token(a, x), row = first + j, h = kvh * g + x - j * g, xs = x - row0;
         if (x >= nrows) continue;
         const size_t at = (size_t)row * a.out_row + (size_t)h * Dh + 4 * lg;
 #pragma unroll
-        for (int f = 0; f < HALF; ++f) {
-            const f32x4_t o = ((kg == 0 ? acc[qt][f] : acc[qt][HALF + f]) * wi + *(const f32x4_t*)(from + (f * 64 + lane) * 4) * wo) * inv;
-            const int ff = kg * HALF + f;
+        for (int f = 0; f < FW; ++f) {
+            f32x4_t o = kg == 0 ? acc[qt][f] : acc[qt][NV - FW + f];
+            if constexpr (KG == 2) o = o * wi + *(const f32x4_t*)(from + (f * 64 + lane) * 4) * wo;
+            o *= inv;
+            const int ff = kg * FW + f;
             if (shared) {
                 *(f32x4_t*)(slot + xs * Dh + 16 * ff + 4 * lg) = o;
             } else if (a.act == FASTCOT_BF16) *(uint2*)((bf16_t*)a.out + at + 16 * ff) = make_uint2(pk_bf16(o[0], o[1]), pk_bf16(o[2], o[3]));
@@ -928,10 +938,10 @@ __global__ __launch_bounds__(256, 1) void k_paged_join(PagedAttnArgs a) {
     }
 }
 
-#define PG_WORKERS 512           // most workgroups of a launch; of those of many rows 256
+#define PG_WORKERS 512           // most workgroups of a launch
 // partial results: two slots a workgroup, of up to 32 rows, or of a unit of many rows
 size_t fc_paged_attn_scratch_bytes(int Dh) {
-    const size_t few = (size_t)PG_WORKERS * 2 * 32, many = (size_t)PG_WORKERS * 64 * many_tiles(Dh / 32);
+    const size_t few = (size_t)PG_WORKERS * 2 * 32, many = (size_t)PG_WORKERS * 2 * 64 * many_tiles(Dh / 32);
     return (few > many ? few : many) * (Dh + 2) * 4;
 }
 
@@ -947,6 +957,23 @@ static hipError_t launch_as(PagedAttnArgs a, int grid, hipStream_t st) {
     kernel<<<grid < PG_WORKERS ? grid : PG_WORKERS, NW * 64, bytes, st>>>(a, (rows + 16 * QT - 1) / (16 * QT));
     return hipGetLastError();
 }
+// Many rows.  bf16 rows: with more units than CUs two workgroups of four waves on every CU, so that one's products go on while the other one is between
+// units (4096 rows of 32 heads under a window of 1024: 146 us with eight waves, 129 so); fewer units find eight waves sooner done (1024 rows from the
+// start of a sequence 38 / 44, 128 rows 16 / 20, 64 rows of 64 heads on 8 over 20000 positions 78 / 82).  fp32 rows, whose lower parts fill the LDS: eight waves.
+template <int G, int QP, int KG>
+static hipError_t launch_many(PagedAttnArgs a, int grid, hipStream_t st) {
+    constexpr int QT = many_tiles(G), RG = many_groups(G, QP), RT = 16 * RG * QT;
+    const size_t stage = KG * 4 * 128 * G * 16, low = many_low(G, QP) ? RG * QT * G * 2 * 1024 : 0, meet = KG == 2 ? 2 * RG * QT * (G * 256 + 128) * 4 : 0;
+    const size_t bytes = stage + low > meet ? stage + low : meet;
+    auto kernel = k_paged_many<G, QT, RG, KG, QP, QP>;
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return e;
+    a.whole = 16;
+    if (grid > PG_WORKERS) grid = PG_WORKERS;
+    kernel<<<grid, 64 * RG * KG, bytes, st>>>(a, (a.r.R * a.g + RT - 1) / RT);
+    k_paged_join<G, RT><<<grid * (RT / 16), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
 // Up to 16 rows: where every unit finds a CU of its own, eight waves share its blocks; with more units two workgroups of four waves on every CU, so that
 // one's loads go on while the other one's waves meet (32 sequences of 100 to 500 positions over 32 heads 36.7 / 31.3 us, 200 of 20 to 300 over 8 heads
 // 41.7 / 32.9; the other way round 7B heads, 8000 positions 26.5 / 26.8, 70B heads, 120000 positions 88 / 100, 7B window of 16, 777 positions 13.3 / 15.8).
@@ -956,18 +983,10 @@ static hipError_t launch(const PagedAttnArgs& a, hipStream_t st) {
     const int cus = fc_num_cus();
     if constexpr (!F32) {
         if (a.r.R * a.g > 32) {
-            constexpr int QT = many_tiles(G), RG = many_groups(G, QP), RT = 16 * RG * QT;
-            const size_t stage = 2 * 4 * 128 * G * 16, low = many_low(G, QP) ? RG * QT * G * 2 * 1024 : 0, meet = 2 * RG * QT * (G * 256 + 128) * 4;
-            const size_t bytes = stage + low > meet ? stage + low : meet;
-            auto kernel = k_paged_many<G, QT, RG, QP, QP>;
-            const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-            if (e != hipSuccess) return e;
-            PagedAttnArgs m = a;
-            m.whole = 16;
-            const int grid = cus < PG_WORKERS / 2 ? cus : PG_WORKERS / 2;
-            kernel<<<grid, 128 * RG, bytes, st>>>(m, (a.r.R * a.g + RT - 1) / RT);
-            k_paged_join<G, RT><<<grid * (RT / 16), 256, 0, st>>>(m);
-            return hipGetLastError();
+            constexpr int RT = 16 * many_groups(G, QP) * many_tiles(G);
+            if constexpr (QP == 1)
+                if ((int64_t)a.r.B * a.c.Hkv * ((a.r.R * a.g + RT - 1) / RT) > cus) return launch_many<G, QP, 1>(a, 2 * cus, st);
+            return launch_many<G, QP, 2>(a, cus, st);
         }
     }
     if (a.r.R * a.g > 16) return launch_as<G, F32, 2, 4, QP, PP>(a, cus, st);

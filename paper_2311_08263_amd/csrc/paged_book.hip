@@ -10,7 +10,7 @@
 #include "gemmco.h"      // fc_num_cus
 
 #define PG_WG 1024
-#define PG_HEAD 16384        // bytes of the scratch in front of the lists: number of moves, at 256 the counters of 512 workgroups, at 8192 units to join of 256
+#define PG_HEAD 16384        // bytes of the scratch in front of the lists: number of moves, at 256 the counters of 512 workgroups, at 4096 their units to join
 #define NONE_FIRST INT_MAX
 
 // exclusive prefix sum over the workgroup; *total: the sum.  lds: 17 ints
@@ -535,7 +535,7 @@ extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const f
     a.out = d_out; a.out_row = out_row_stride; a.lse = d_lse;
     a.H = n_heads; a.act = act_dtype; a.g = n_heads / c->n_kv_heads; a.g_inv = (uint32_t)(((1ull << 32) + a.g - 1) / a.g); a.esz = (int32_t)esz_of(c); a.window = window; a.sinks = sinks;
     a.cnt = (int32_t*)d_scratch + 64;
-    a.joins = (PagedJoin*)((char*)d_scratch + 8192);
+    a.joins = (PagedJoin*)((char*)d_scratch + 4096);
     a.part = (float*)((char*)d_scratch + PG_HEAD + 3 * list_bytes(c));
     return launched(name, fc_paged_attn(a, (hipStream_t)hip_stream));
 }
