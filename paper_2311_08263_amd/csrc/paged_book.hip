@@ -290,31 +290,27 @@ __global__ __launch_bounds__(256) void k_paged_reset(PagedView c) {
     for (size_t i = i0; i < (size_t)c.N; i += step) c.ref[i] = 0;
 }
 
-template <typename A> __device__ inline float pg_value(A x) { if constexpr (sizeof(A) == 2) return bf16_to_f32(x); else return x; }
-// eight values next to each other
-template <typename A> __device__ inline void pg_load8(const A* p, float* v) {
-    if constexpr (sizeof(A) == 2) {
-        const uint4 u = *(const uint4*)p;
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+typedef __attribute__((__vector_size__(16))) uint32_t pg_u32x4;
+// eight values next to each other, in the cache's type: one or two pieces of 16 bytes
+template <typename T, typename A> __device__ inline void pg_load8(const A* p, pg_u32x4* to) {
+    if constexpr (sizeof(A) == sizeof(T)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(w[e] << 16); v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
+        for (unsigned w = 0; w < sizeof(T) / 2; ++w) to[w] = ((const pg_u32x4*)p)[w];
     } else {
         const float4 x = *(const float4*)p, y = *(const float4*)(p + 4);
-        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        to[0] = (pg_u32x4){pk_bf16(x.x, x.y), pk_bf16(x.z, x.w), pk_bf16(y.x, y.y), pk_bf16(y.z, y.w)};
     }
 }
-template <typename T> __device__ inline void pg_store8(T* p, const float* v) {
-    if constexpr (sizeof(T) == 2) *(uint4*)p = make_uint4(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7]));
-    else { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]); }
-}
 
-// New rows into the pages, a workgroup per block of 32 positions and K/V head (grid: x over blocks and heads, y over sequences).  Threads go by what they store,
-// whole 16-byte pieces in the order of the block (V: eight positions of a head element; pieces that the rows fill in part, value by value), so stores are
-// whole lines and what a line of the rows is read for twice comes out of the L1.  Bound by HBM, one token of each sequence by latency.  (A thread per eight
-// elements of a row, V stored value by value: 4096 fp32 rows of 32 heads 143 us.)
+// New rows into the pages, a workgroup per block of 32 positions and K/V head (grid: x over blocks and heads, y over sequences): rows come in whole lines,
+// meet in LDS in the cache's type, and go out in the order of the block, in 16-byte pieces of whole lines (V: eight positions of a head element; pieces that
+// the rows fill in part, value by value).  Bound by HBM, one token of each sequence by latency.  4096 fp32 rows of 32 heads, not in the caches: threads by
+// eight elements of a row 143 us, by what they store without the LDS 56.
 template <typename T, typename A>
 __global__ __launch_bounds__(256) void k_paged_write(PagedView c, PagedRows r, T* kl, T* vl, const A* k, const A* v, int64_t row_stride) {
-    const int i = blockIdx.y, s = pg_seq(r, c, i), G = c.Dh >> 5, tid = threadIdx.x;
+    constexpr int E = 16 / sizeof(T), W = sizeof(T) / 2;       // values of a piece, pieces of eight values
+    extern __shared__ __align__(16) char lds[];
+    const int i = blockIdx.y, s = pg_seq(r, c, i), G = c.Dh >> 5, D8 = c.Dh >> 3, tid = threadIdx.x;
     if (s < 0) return;
     int first, count;
     pg_rows(r, i, first, count);
@@ -323,35 +319,38 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedView c, PagedRows r, T
     if (p0 >= n + count || slot >= c.MP) return;
     const int page = c.table[(size_t)s * c.MP + slot];
     if (pg_none(c, page)) return;
-    const size_t base = ((((size_t)page * c.Hkv + h) << c.pb) + (blk & ((1 << c.pb) - 1))) * 32 * c.Dh;
-    const A* kr = k + (int64_t)(first + p0 - n) * row_stride + (size_t)h * c.Dh;       // the row of position p0 (which may lie in front of the first one)
-    const A* vr = v + (int64_t)(first + p0 - n) * row_stride + (size_t)h * c.Dh;
     const int lo = n - p0 > 0 ? n - p0 : 0, hi = n + count - p0 < 32 ? n + count - p0 : 32;          // positions of the block that are written
-    for (int x = tid; x < 32 * G; x += 256) {                  // a position and 32 elements: one piece of four fragments each
-        const int t = x / (16 * G), y = x % (16 * G), q = y & 15, p = 8 * (q >> 2) + 4 * t + (q & 3);
-        if (p < lo || p >= hi) continue;
+    const int LR = c.Dh + E;                                   // values of a row in LDS (one piece more: the rows begin on different banks)
+    T* kt = (T*)lds; T* vt = kt + 32 * LR;
+    for (int x = tid + lo * D8; x < hi * D8; x += 256) {
+        const int p = x / D8, d = 8 * (x - p * D8);
+        const int64_t at = (int64_t)(first + p0 + p - n) * row_stride + (int64_t)h * c.Dh + d;
+        pg_u32x4 a[W], b[W];
+        pg_load8<T>(k + at, a);
+        pg_load8<T>(v + at, b);
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            float a[8];
-            pg_load8(kr + p * row_stride + 32 * (y >> 4) + 8 * f, a);
-            pg_store8(kl + base + (size_t)((t * 4 + f) * 16 * G + y) * 8, a);
-        }
+        for (int w = 0; w < W; ++w) { *(pg_u32x4*)(kt + p * LR + d + w * E) = a[w]; *(pg_u32x4*)(vt + p * LR + d + w * E) = b[w]; }
     }
-    for (int x = tid; x < 4 * c.Dh; x += 256) {
-        const int d = (x >> 6) * 16 + (x & 15), p = 8 * (x >> 4 & 3);
-        T* to = vl + base + (size_t)x * 8;
-        float a[8];
-        if (p >= lo && p + 8 <= hi) {
+    __syncthreads();
+    const size_t base = ((((size_t)page * c.Hkv + h) << c.pb) + (blk & ((1 << c.pb) - 1))) * 32 * c.Dh;
+    for (int x = tid; x < 4 * c.Dh; x += 256) {                // eights of the block, in its order
+        T* kd = kl + base + (size_t)x * 8; T* vd = vl + base + (size_t)x * 8;
+        // K: t, s, then 16 positions of each of the head's 32s
+        const int y = x % (16 * G), ts = x / (16 * G), q = y & 15, p = 8 * (q >> 2) + 4 * (ts >> 2) + (q & 3), d = 32 * (y >> 4) + 8 * (ts & 3);
+        if (p >= lo && p < hi)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = pg_value(vr[(p + e) * row_stride + d]);
-            pg_store8(to, a);
+            for (int w = 0; w < W; ++w) __builtin_nontemporal_store(*(const pg_u32x4*)(kt + p * LR + d + w * E), (pg_u32x4*)kd + w);
+        // V: sixteen head elements, then four times eight positions of them
+        const int e0 = (x >> 6) * 16 + (x & 15), v0 = 8 * (x >> 4 & 3);
+        if (v0 >= lo && v0 + 8 <= hi) {
+            alignas(16) T z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = vt[(v0 + e) * LR + e0];
+#pragma unroll
+            for (int w = 0; w < W; ++w) __builtin_nontemporal_store(*(const pg_u32x4*)(z + w * E), (pg_u32x4*)vd + w);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (p + e < lo || p + e >= hi) continue;
-                const float y = pg_value(vr[(p + e) * row_stride + d]);
-                if constexpr (sizeof(T) == 2) to[e] = (T)(pk_bf16(y, 0.f) & 0xFFFF); else to[e] = y;
-            }
+            for (int e = 0; e < 8; ++e) if (v0 + e >= lo && v0 + e < hi) vd[e] = vt[(v0 + e) * LR + e0];
         }
     }
 }
@@ -504,11 +503,14 @@ extern "C" int fastcot_paged_write(const fastcot_paged* c, int32_t layer, const 
     const int64_t gx = ((int64_t)(r.R + 31) / 32 + 1) * c->n_kv_heads;             // (rows may begin inside a block)
     if (gx > 0x7FFFFFFF) FAIL(FASTCOT_ECAPACITY, "%s: too many rows of one sequence", name);
     const dim3 grid((unsigned)gx, (unsigned)r.B);
+    const size_t lds = 2 * 32 * (c->head_dim * esz_of(c) + 16);
     hipStream_t st = (hipStream_t)hip_stream;
-    if (c->dtype == FASTCOT_F32) k_paged_write<float, float><<<grid, 256, 0, st>>>(v, r, (float*)kl, (float*)vl, (const float*)d_k, (const float*)d_v, row_stride);
+    if (lds > 65536)                                           // (fp32 heads of 256: more than 64 KB have to be asked for)
+        TRY(launched(name, hipFuncSetAttribute((const void*)k_paged_write<float, float>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)));
+    if (c->dtype == FASTCOT_F32) k_paged_write<float, float><<<grid, 256, lds, st>>>(v, r, (float*)kl, (float*)vl, (const float*)d_k, (const float*)d_v, row_stride);
     else if (act_dtype == FASTCOT_F32)
-        k_paged_write<bf16_t, float><<<grid, 256, 0, st>>>(v, r, (bf16_t*)kl, (bf16_t*)vl, (const float*)d_k, (const float*)d_v, row_stride);
-    else k_paged_write<bf16_t, bf16_t><<<grid, 256, 0, st>>>(v, r, (bf16_t*)kl, (bf16_t*)vl, (const bf16_t*)d_k, (const bf16_t*)d_v, row_stride);
+        k_paged_write<bf16_t, float><<<grid, 256, lds, st>>>(v, r, (bf16_t*)kl, (bf16_t*)vl, (const float*)d_k, (const float*)d_v, row_stride);
+    else k_paged_write<bf16_t, bf16_t><<<grid, 256, lds, st>>>(v, r, (bf16_t*)kl, (bf16_t*)vl, (const bf16_t*)d_k, (const bf16_t*)d_v, row_stride);
     return launched(name, hipGetLastError());
 }
 extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const fastcot_paged_rows* rows, const void* d_q, int64_t q_row_stride,

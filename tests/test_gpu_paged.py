@@ -182,7 +182,8 @@ def test_attention_strides(fc):
 
 @pytest.mark.parametrize("lens,rows,P,Hkv,Dh,cache,act", [
     ([0, 31, 40], [1, 1, 1], 32, 2, 128, "bf16", "bf16"), ([5, 64], [70, 3], 64, 1, 96, "bf16", "f32"), ([1, 30], [7, 8], 32, 4, 64, "f32", "f32"),
-    ([0], [200], 128, 2, 256, "bf16", "f32"), ([3], [129], 32, 1, 32, "bf16", "bf16"), ([8, 16], [24, 40], 32, 3, 192, "f32", "f32")])
+    ([0], [200], 128, 2, 256, "bf16", "f32"), ([3], [129], 32, 1, 32, "bf16", "bf16"), ([8, 16], [24, 40], 32, 3, 192, "f32", "f32"),
+    ([31, 2], [2, 40], 64, 2, 256, "f32", "f32")])
 def test_write(fc, lens, rows, P, Hkv, Dh, cache, act):
     """Rows at any offset inside a page; values that fp32 rounds up and down; a row without a page is dropped, nothing else changes."""
     import torch
