@@ -437,6 +437,7 @@ __global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_at
         }
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
+#pragma clang fp contract(off)           // (a score meets the maximum in its own rounding)
             f32x4_t sc[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {

@@ -382,6 +382,7 @@ static int view_of(const char* name, const fastcot_paged* c, PagedView* v) {
 static int entries_of(const char* name, const fastcot_paged* c, int32_t count, const void* a, const void* b) {
     if (count < 0 || count > c->max_seqs) FAIL(FASTCOT_EINVAL, "%s: count %d outside 0..max_seqs", name, (int)count);
     if (count && (!a || !b)) FAIL(FASTCOT_EINVAL, "%s: NULL device pointer", name);
+    if (((uintptr_t)a | (uintptr_t)b) & 3) FAIL(FASTCOT_EINVAL, "%s: misaligned int32 array", name);
     return 0;
 }
 static int scratch_of(const char* name, void* d_scratch) {
@@ -393,6 +394,7 @@ static int rows_of(const char* name, const fastcot_paged_rows* r, int32_t layer,
     if (r->n_seqs > 65535) FAIL(FASTCOT_EINVAL, "%s: more than 65535 sequences", name);
     if (!r->d_seqs && r->n_seqs > c->max_seqs) FAIL(FASTCOT_EINVAL, "%s: more sequences than the cache has", name);
     if (!r->d_row_start && (int64_t)r->n_seqs * r->rows != r->n_rows) FAIL(FASTCOT_EINVAL, "%s: n_rows is not n_seqs * rows", name);
+    if (((uintptr_t)r->d_seqs | (uintptr_t)r->d_row_start) & 3) FAIL(FASTCOT_EINVAL, "%s: misaligned int32 array", name);
     if (layer < 0 || layer >= c->n_layers) FAIL(FASTCOT_EINVAL, "%s: layer %d outside the cache", name, (int)layer);
     if (act != FASTCOT_F32 && act != FASTCOT_BF16) FAIL(FASTCOT_EINVAL, "%s: unknown type of rows", name);
     if (act == FASTCOT_BF16 && c->dtype == FASTCOT_F32) FAIL(FASTCOT_EINVAL, "%s: an fp32 cache takes fp32 rows", name);
@@ -528,6 +530,7 @@ extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const f
     const double g = n_heads / c->n_kv_heads, tiles = (a.r.R * g + 15) / 16, blocks = (double)c->max_pages * (c->page_size / 32) + a.r.R / 32 + 10;
     if (a.r.R * g >= (1 << 26) || (double)a.r.B * c->n_kv_heads * tiles * blocks >= 2147483648.0)
         FAIL(FASTCOT_ECAPACITY, "%s: rows times positions of the table pass 2^31 blocks", name);
+    if ((uintptr_t)d_lse & 3) FAIL(FASTCOT_EINVAL, "%s: misaligned d_lse", name);
     if (!d_q || !d_out || (((uintptr_t)d_q | (uintptr_t)d_out) & 15)) FAIL(FASTCOT_EINVAL, "%s: queries and output have to be given, aligned to 16 bytes", name);
     if (q_row_stride % 8 || q_head_stride % 8 || q_row_stride < 0 || q_head_stride < 0) FAIL(FASTCOT_EINVAL, "%s: strides of the queries are no multiples of 8", name);
     if (out_row_stride % 8 || out_row_stride < (int64_t)n_heads * c->head_dim) FAIL(FASTCOT_EINVAL, "%s: row stride of the output below a row or no multiple of 8", name);

@@ -122,7 +122,7 @@ def test_attention(fc, lens, rows, P, H, Hkv, Dh, cache, act, window, sinks):
         assert (out == c.attn(q, seqs=ints(slots), window=window, sinks=sinks)).all()
 
 
-@pytest.mark.parametrize("H,Hkv,rows,window,sinks", [(4, 4, [6, 1, 20], 0, 0), (8, 2, [16, 9, 3], 45, 3)])
+@pytest.mark.parametrize("H,Hkv,rows,window,sinks", [(4, 4, [6, 1, 9], 0, 0), (4, 4, [6, 1, 20], 0, 0), (8, 2, [16, 9, 3], 45, 3), (2, 1, [100, 7, 70], 0, 0)])
 @pytest.mark.parametrize("cache,act", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
 def test_attention_takes_nothing_from_hidden_positions(fc, H, Hkv, rows, window, sinks, cache, act):
     """V holds an infinity and a NaN where only some of a unit's rows see them, and NaN wherever nobody has written; pages are missing in the
@@ -152,19 +152,124 @@ def test_attention_takes_nothing_from_hidden_positions(fc, H, Hkv, rows, window,
     check(out[:-2], lse[:-2], (want[:-2], wlse[:-2]), act)
 
 
-def test_attention_at_the_ends_of_the_range(fc):
-    """Queries up to the largest fp32 number, and rows all of whose scores lie far below zero."""
+@pytest.mark.parametrize("rows", [3, 80])
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_attention_at_the_ends_of_the_range(fc, rows, act):
+    """Queries up to the largest numbers, and rows all of whose scores lie far below zero or far above."""
     import torch
-    say("paged attention at the ends of the range")
-    c, slots = make(fc, [90], [3], 32, 2, 128)
-    q = queries([3], 4, 128, "f32")
-    for scale_q, scale_k in ((3e38 / 1.5, 1e-30), (1e18, 1e15)):
-        qq = torch.sign(q) * scale_q if scale_q > 1e30 else q.abs() * scale_q
-        c2, _ = make(fc, [90], [3], 32, 2, 128)
-        c2.k.copy_((c.k.float() * scale_k if scale_q > 1e30 else -c.k.float().abs() * scale_k).bfloat16())
+    say(f"paged attention at the ends of the range rows={rows} {act}")
+    c, slots = make(fc, [90], [rows], 32, 2, 128)
+    q = queries([rows], 4, 128, "f32")
+    for scale_q, scale_k in ((3e38 / 1.5, 1e-30), (1e18, -1e15), (1e18, 1e15)):
+        qq = (torch.sign(q) * scale_q if scale_q > 1e30 else q.abs() * scale_q).to(torch.float32 if act == "f32" else torch.bfloat16)
+        c2, _ = make(fc, [90], [rows], 32, 2, 128)
+        c2.k.copy_((c.k.float() * scale_k if scale_q > 1e30 else c.k.float().abs() * scale_k).bfloat16())
         out, lse = c2.attn(qq, seqs=ints(slots), want_lse=True)
-        want, wl = Plain(c2).attn(128, 0, slots, [3], qq, 0, 0)
-        assert rel(out, want) < 2e-6 and rel(lse, wl) < 2e-6
+        want, wl = dense(c2, slots, [rows], qq, 0, 0)
+        assert rel(out, want) < (2e-6 if act == "f32" else 2 ** -8 + 2 ** -16) and rel(lse, wl) < 2e-6
+
+
+def test_one_sequence_twice(fc):
+    """Two passes of a sequence in one call (drafts that share its pages): each gets its own result."""
+    import torch
+    say("paged attention, a sequence twice")
+    c, slots = make(fc, [300, 40], [2, 2], 32, 2, 128)
+    q = queries([6], 4, 128, "f32")
+    out = c.attn(q, seqs=ints([slots[0], slots[1], slots[0]]))
+    assert torch.equal(out[:2], c.attn(q[:2].contiguous(), seqs=ints(slots[:1]))) and rel(out, Plain(c).attn(128, 0, [slots[0], slots[1], slots[0]], [2, 2, 2], q, 0, 0)[0]) < 2e-6
+
+
+def test_pools_of_more_than_four_gigabytes(fc):
+    """Pages behind the 32-bit offsets of bytes and of values: written, read by both kernels, shared, copied and moved."""
+    import torch
+    say("paged cache of 2 x 9.8 GB")
+    N, P, Dh = 300000, 32, 256
+    c = fc.PagedCache(N, P, 2, Dh, max_seqs=3, max_pages=8)
+    c.ref[:N - 9] = 1                                  # all but the last nine pages are taken
+    rows = [100, 100]
+    seqs = ints([2, 0])
+    assert c.grow(seqs, ints(rows)).tolist() == [0, 0] and int(c.table[c.table >= 0].min()) == N - 9
+    k, v, q = (queries(rows, 2, Dh, "bf16", i) for i in (1, 2, 3))
+    c.write(k, v, seqs=seqs)
+    assert c.advance(seqs, ints([50, 50])).tolist() == [0, 0]
+
+    def check_rows(slot, a):
+        pages = c.table[slot, :4].long()
+        for pool, x, which in ((c.k, k, 0), (c.v, v, 1)):
+            assert torch.equal(canonical(pool[:, pages], Dh)[which][0].transpose(1, 2).reshape(-1, 2, Dh)[:100], x[a:a + 100])
+        for n in (1, 40):                              # one row and many, each at a position that has been written
+            out = c.attn(q[a:a + n], seqs=ints([slot])).view(n, 2, Dh)
+            hidden = torch.arange(50 + n, device="cuda") > torch.arange(50, 50 + n, device="cuda")[:, None]
+            for h in (0, 1):
+                score = (q[a:a + n, h].double() @ k[a:a + 50 + n, h].double().T / Dh ** 0.5).masked_fill(hidden, -torch.inf)
+                assert rel(out[:, h], torch.softmax(score, 1) @ v[a:a + 50 + n, h].double()) < 2 ** -8 + 2 ** -16
+    check_rows(2, 0)
+    check_rows(0, 100)
+    assert c.fork(ints([2]), ints([1])).tolist() == [0] and int(c.table[1, 1]) == N - 1 and int(c.table[1, 0]) == int(c.table[2, 0])
+    one, two = canonical(c.k[:, [int(c.table[2, 1]), N - 1]], Dh)[0][0]
+    assert torch.equal(one[:, :18], two[:, :18])
+    c.ref[:N - 9] = 0
+    used = int(c.compact())
+    assert used == 9 and int(c.table.max()) == 8 and int(c.ref[:9].min()) >= 1 and int(c.ref[9:].max()) == 0
+    check_rows(2, 0)
+
+
+def test_refusals_of_the_binding(fc):
+    """What the binding refuses before the library sees it."""
+    import torch
+    say("paged cache, refusals of the binding")
+    c, slots = make(fc, [40, 7], [5, 5], 64, 2, 128)
+    s, q = ints(slots), queries([10], 4, 128, "f32")
+    k = queries([10], 2, 128, "f32")
+
+    def refused(call, text):
+        with pytest.raises(fc.FastcotError, match=text) as e:
+            call()
+        assert e.value.rc == -1
+    refused(lambda: c.grow(s.cpu(), s), "seqs")
+    refused(lambda: c.grow(s.long(), s), "seqs")
+    refused(lambda: c.grow(s, s[:1]), "rows")
+    refused(lambda: c.fork(s, ints([1, 2, 3])), "dst")
+    refused(lambda: c.trim(s[None], 5), "seqs")
+    refused(lambda: c.free(ints([0, 1, 2, 3])[::2]), "seqs")
+    refused(lambda: c.trim(s, 0), "window")
+    refused(lambda: c.attn(q[:9], seqs=s), "row_start")
+    refused(lambda: c.attn(q.cpu(), seqs=s), "q:")
+    refused(lambda: c.attn(q.half(), seqs=s), "q:")
+    refused(lambda: c.attn(q[..., :64], seqs=s), "q:")
+    refused(lambda: c.attn(q.transpose(1, 2).contiguous().transpose(1, 2), seqs=s), "q:")
+    refused(lambda: c.attn(queries([10], 3, 128, "f32"), seqs=s), "heads")
+    refused(lambda: c.attn(q, seqs=s, out=torch.empty(10, 512, dtype=torch.bfloat16, device="cuda")), "out")
+    refused(lambda: c.attn(q, seqs=s, scratch=c.scratch[:256]), "scratch")
+    refused(lambda: c.attn(q, seqs=s, row_start=ints([0, 10])), "row_start")
+    refused(lambda: c.attn(q, layer=1, seqs=s), "layer")
+    refused(lambda: c.write(k, k.bfloat16(), seqs=s), "differ")
+    refused(lambda: c.write(k, k[:8], seqs=s), "differ")
+    refused(lambda: c.write(q[:, ::2], q[:, ::2], seqs=s), "follow")
+    refused(lambda: c.write(k, torch.cat([k, k], 1)[:, :2], seqs=s), "strides")
+    for bad in (dict(page_size=48), dict(head_dim=80), dict(dtype=torch.float16), dict(book=torch.zeros(5, dtype=torch.int32, device="cuda")),
+                dict(k=torch.zeros(1, 10, 2, 2, 4096, device="cuda"))):
+        refused(lambda: fc.PagedCache(**{**dict(n_pages=10, page_size=64, n_kv_heads=2, head_dim=128), **bad}), None)
+    assert c.attn(q[:0], seqs=s[:0]).shape == (0, 512) and c.grow(s[:0], s[:0]).numel() == 0
+
+
+def test_on_another_stream(fc):
+    """The calls go to the stream that is current, and wait for nobody else's."""
+    import torch
+    say("paged cache on another stream")
+    c, slots = make(fc, [100], [3], 32, 2, 128)
+    q, s = queries([3], 4, 128, "f32"), ints(slots)
+    want = c.attn(q, seqs=s)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device="cuda")
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            big = big @ big * 1e-4
+        qq = q * (big[0, 0] * 0 + 1)                   # ready only when the side stream has come here
+        out = c.attn(qq, seqs=s)
+    side.synchronize()
+    assert torch.equal(out, want)
 
 
 def test_attention_strides(fc):

@@ -27,7 +27,14 @@ def test_sizes():
     assert L.fastcot_paged_scratch_bytes(ctypes.byref(desc())) > 0
 
 
-BAD = [dict(n_layers=0), dict(n_pages=0), dict(n_pages=(1 << 24) + 1), dict(page_size=16), dict(page_size=48), dict(page_size=8192), dict(n_kv_heads=0),
+def test_more_blocks_than_31_bits_count():
+    """Rows times positions of the table, which the kernel deals out by number."""
+    r = PagedRows(3, 1 << 20, 3 << 20, None, None)
+    assert attn(d=desc(max_pages=1 << 24), r=r) == -3 and b"2^31" in binding.lib().fastcot_last_error(None)
+    assert attn(r=PagedRows(1, 1 << 26, 1 << 26, None, None)) == -3
+
+
+BAD = [dict(n_layers=4096, n_kv_heads=4096, page_size=4096), dict(n_layers=0), dict(n_pages=0), dict(n_pages=(1 << 24) + 1), dict(page_size=16), dict(page_size=48), dict(page_size=8192), dict(n_kv_heads=0),
        dict(head_dim=100), dict(head_dim=160), dict(dtype=2), dict(max_seqs=0), dict(max_seqs=4097), dict(max_pages=0), dict(max_pages=1 << 25)]
 
 
@@ -60,6 +67,7 @@ def test_entries():
         refused(L.fastcot_paged_free(d, count, 4096, None, None), b"count")
         refused(L.fastcot_paged_trim(d, count, 4096, 5, 0, None, None), b"count")
     refused(L.fastcot_paged_grow(d, 1, None, 4096, None, 4096, None), b"NULL")
+    refused(L.fastcot_paged_grow(d, 1, 4097, 4096, None, 4096, None), b"misaligned")
     refused(L.fastcot_paged_advance(d, 1, 4096, None, None, None), b"NULL")
     refused(L.fastcot_paged_grow(d, 1, 4096, 4096, None, None, None), b"scratch")
     refused(L.fastcot_paged_fork(d, 1, 4096, 4096, None, None, None), b"scratch")
@@ -91,6 +99,8 @@ def test_rows(call):
     refused(call(r=PagedRows(3, 2, 7, None, None)), b"n_rows")
     refused(call(r=PagedRows(4, 1, 4, None, None)), b"more sequences")
     refused(call(r=PagedRows(70000, 1, 70000, 4096, None)), b"65535")
+    refused(call(r=PagedRows(3, 2, 6, 4098, None)), b"misaligned")
+    refused(call(r=PagedRows(3, 2, 6, 4096, 4097)), b"misaligned")
     refused(call(layer=2), b"layer")
     refused(call(layer=-1), b"layer")
     refused(call(act=3), b"type")
