@@ -48,7 +48,8 @@ struct PagedAttnArgs {
     int32_t H, act;                        // act: 0 fp32, 1 bf16 rows
     int32_t g; uint32_t g_inv;             // query heads of a K/V head, and 2^32 / g rounded up
     int32_t esz;                           // bytes of a cached value
-    int32_t window, sinks;                 // window 0: none
+    int32_t window, sinks;                 // window 0: none, and no sinks
+    uint32_t reach;                        // a row sees what lies less far back: the window, or 2^31
     int32_t whole;                         // most blocks of a unit that is not cut
     int32_t* cnt; PagedJoin* joins; float* part;       // hand-off of parts: counters (zero between launches), units to join, partial results
 };

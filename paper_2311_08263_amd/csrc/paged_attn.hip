@@ -54,7 +54,17 @@ __device__ inline void pg_far(float* p, float& by, float& from) {
     by = 1.f; from = 0.f;
 }
 __device__ inline bool pg_sees(const PagedAttnArgs& a, int key, int pos) {
-    return key <= pos && (!a.window || key > pos - a.window || key < a.sinks);
+    return (uint32_t)(pos - key) < a.reach || (key < a.sinks && key <= pos);
+}
+// scores p of positions key .. key + 7 for a row at position pos: what it does not see becomes -infinity.  sunk: some of them are among the sinks
+__device__ inline void pg_mask8(const PagedAttnArgs& a, int key, int pos, bool sunk, float* p) {
+    if (sunk) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = pg_sees(a, key + e, pos) ? p[e] : -INFINITY;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (uint32_t)(pos - key - e) < a.reach ? p[e] : -INFINITY;
+    }
 }
 // whether any of eight bf16 values is not finite (their exponents are all ones: a carry out of each when the lowest bit is added)
 __device__ inline bool pg_not_finite(const u32x4_t& v) {
@@ -459,10 +469,7 @@ __global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_at
             float p[8], bm = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[e] = !F32 && QP == 1 ? sc[e >> 2][e & 3] * scale2 : sc[e >> 2][e & 3];
-            if (!whole) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = pg_sees(a, kb + 8 * lg + e, pos[qt]) ? p[e] : -INFINITY;
-            }
+            if (!whole) pg_mask8(a, kb + 8 * lg, pos[qt], kb < a.sinks, p);
 #pragma unroll
             for (int e = 0; e < 8; ++e) bm = fmaxf(bm, p[e]);
             bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
@@ -736,10 +743,9 @@ __global__ __launch_bounds__(64 * RG * KG, many_waves(G, QP)) void k_paged_many(
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[qt][e] = sc[qt][e >> 2][e & 3];
         if (!whole) {
+            const bool sunk = kb < a.sinks;
 #pragma unroll
-            for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[qt][e] = pg_sees(a, kb + 8 * lg + e, pos[qt]) ? p[qt][e] : -INFINITY;
+            for (int qt = 0; qt < QT; ++qt) pg_mask8(a, kb + 8 * lg, pos[qt], sunk, p[qt]);
         }
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {

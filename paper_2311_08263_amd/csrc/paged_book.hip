@@ -538,7 +538,7 @@ extern "C" int fastcot_paged_attn(const fastcot_paged* c, int32_t layer, const f
     a.vl = a.c.v + (size_t)layer * c->n_pages * page_bytes(c);
     a.q = d_q; a.q_row = q_row_stride; a.q_head = q_head_stride;
     a.out = d_out; a.out_row = out_row_stride; a.lse = d_lse;
-    a.H = n_heads; a.act = act_dtype; a.g = n_heads / c->n_kv_heads; a.g_inv = (uint32_t)(((1ull << 32) + a.g - 1) / a.g); a.esz = (int32_t)esz_of(c); a.window = window; a.sinks = sinks;
+    a.H = n_heads; a.act = act_dtype; a.g = n_heads / c->n_kv_heads; a.g_inv = (uint32_t)(((1ull << 32) + a.g - 1) / a.g); a.esz = (int32_t)esz_of(c); a.window = window; a.sinks = window ? sinks : 0; a.reach = window ? (uint32_t)window : 0x80000000u;
     a.cnt = (int32_t*)d_scratch + 64;
     a.joins = (PagedJoin*)((char*)d_scratch + 4096);
     a.part = (float*)((char*)d_scratch + PG_HEAD + 3 * list_bytes(c));
