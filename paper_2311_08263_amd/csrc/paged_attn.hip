@@ -585,13 +585,19 @@ static constexpr int many_tiles(int G) { return G > 4 ? 1 : 2; }
 static constexpr int many_groups(int G, int QP) { return G == 8 && QP == 3 ? 2 : 4; }
 static constexpr int many_waves(int G, int QP) { return G == 8 && QP == 3 ? 1 : 2; }
 static constexpr bool many_low(int G, int QP) { return G < 8 && QP == 3; }
-// Many rows of a sequence (prompt chunks, wide windows, windows over grouped heads; bf16 caches): 64 * QT rows a unit.  Four waves of 16 * QT rows take the even
-// blocks, four with the same rows the odd ones; a pair of blocks goes global -> LDS while the previous pair is used, so that K and V are
-// read once for all the unit's rows and a fragment from LDS once for a wave's QT tiles.  At the end the two waves of the same rows exchange half of their sums.
-// Bound: matrix instructions (16 of 16 x 16 x 32 for a tile and block with bf16 rows, 48 with fp32 rows) beside about 30 vector instructions and 8
-// exponentials for bf16 rows.  To keep those few, sums are taken relative to a reference that moves only when a score passes it by 8 powers of two (so
-// weights are at most 2^8, and nothing is rescaled in most blocks).  With bf16 rows the weights are rounded to bf16 once in front of the product
-// with V: as large an error as the rounding of the output, half a step of each weight; their sum is taken before the rounding.
+// Many rows of a sequence (prompt chunks, wide windows, windows over grouped heads; bf16 caches): 16 * RG * QT rows a unit, RG waves of QT tiles each, or KG = 2
+// times as many, the one half for the even blocks and the other for the odd ones.  The next block (KG of them) goes global -> LDS while the present one is
+// used, so that K and V are read once for all the unit's rows and a fragment from LDS once for a wave's QT tiles.  Two waves of the same rows exchange half of
+// their sums at the end.  Units that several workgroups share are joined by a launch of its own (k_paged_join).
+// Sums are taken relative to a reference that moves only when a score passes it by 8 powers of two: weights are at most 2^8, and in most blocks nothing is
+// rescaled.  With bf16 rows the weights are rounded to bf16 once in front of the product with V: as large an error as the rounding of the output, half a
+// step of each weight; their sum is taken before the rounding.
+// V is multiplied as it is; only where a sum comes out not finite the part is walked once more, carefully (checked in every block, infinities and NaN in V
+// cost 3 % of a long walk).
+// Bound: per block and tile 16 matrix instructions (bf16 rows; 48 with fp32 rows) beside about 30 vector instructions and 8 exponentials, and a kilobyte out of
+// LDS for every two (six) matrix instructions of a wave.  1024 bf16 rows of 32 heads over 20000 positions: 735 TFLOP/s, matrix pipes busy 32 % of the
+// cycles, LDS 42, vector unit 38; fp32 rows 365, times three parts 1100, of 1333 that a large product reaches.  Two waves on a SIMD do not fill each other's
+// waits, and what would help does not find its registers: three tiles a wave 686, two blocks at a time 703 (both spill), four tiles and one wave a SIMD 454.
 template <int G, int QT, int RG, int KG, int QP, int PP>
 __global__ __launch_bounds__(64 * RG * KG, many_waves(G, QP)) void k_paged_many(PagedAttnArgs a, int tiles) {
     constexpr int Dh = 32 * G, NV = 2 * G, RT = 16 * RG * QT, SEC = 128 * G, T = 64 * RG * KG;    // SEC: 16-byte words of one block of K or V
