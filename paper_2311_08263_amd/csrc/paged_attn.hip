@@ -210,8 +210,10 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
     // the sequence that place d.at falls into, the places in front of it, and those of one of its heads
     uint32_t before = 0, head = 0;
     int b = 0, from = 0;                                       // from: a lane that has looked at it
+    // (each walk also ends where the numbers end: lengths that change under a call give wrong results, not an endless one)
     if (by_seq) {
         for (;; b += 64) {
+            if (b >= a.r.B) return false;
             if (a.r.B > 64) { mine = places(b + lane, 0, tiles) * Hkv; incl = pg_wave_scan(mine); }
             const uint64_t hit = __ballot(before + incl > d.at);
             if (hit) {
@@ -227,6 +229,7 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
         }
     } else {
         for (;; ++b) {
+            if (b >= a.r.B) return false;
             mine = 0;
             for (int t = 0; t < tiles; t += 64) mine += places(b, t + lane, t + lane + 1);
             head = pg_lane(pg_wave_scan(mine), 63);
@@ -242,12 +245,14 @@ template <int RT> __device__ inline bool pg_deal(const PagedAttnArgs& a, int til
     p.tile = 0;
     if (by_seq) {
         for (;; ++p.tile) {
+            if (p.tile >= tiles) return false;
             p.blocks = pg_blocks<RT>(a, p.seq, p.n, p.rows, p.tile);
             if (before + p.blocks + PG_UNIT > d.at) break;
             before += p.blocks + PG_UNIT;
         }
     } else {
         for (int t = 0;; t += 64) {
+            if (t >= tiles) return false;
             mine = pg_blocks<RT>(a, p.seq, p.n, p.rows, t + lane);
             if (mine) mine += PG_UNIT;
             incl = pg_wave_scan(mine);
@@ -277,7 +282,7 @@ template <int RT> __device__ inline bool pg_next(const PagedAttnArgs& a, const P
         if (++p.kvh == a.c.Hkv) {
             p.kvh = 0;
             do {
-                ++p.b;
+                if (++p.b >= a.r.B) return false;
                 pg_load(a, p.b, p.seq, p.n, p.first, p.rows);
                 p.seq = pg_uniform(p.seq); p.n = pg_uniform(p.n); p.first = pg_uniform(p.first); p.rows = pg_uniform(p.rows);
             } while (p.rows == 0);
@@ -469,7 +474,7 @@ __global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_at
             float p[8], bm = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[e] = !F32 && QP == 1 ? sc[e >> 2][e & 3] * scale2 : sc[e >> 2][e & 3];
-            if (!whole) pg_mask8(a, kb + 8 * lg, pos[qt], kb < a.sinks, p);
+            if (!whole) pg_mask8(a, kb + 8 * lg, pos[qt], F32 || kb < a.sinks, p);          // (fp32: no registers for two forms)
 #pragma unroll
             for (int e = 0; e < 8; ++e) bm = fmaxf(bm, p[e]);
             bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
