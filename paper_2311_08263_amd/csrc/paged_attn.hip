@@ -995,19 +995,23 @@ static hipError_t launch_many(PagedAttnArgs a, int grid, hipStream_t st) {
 // Up to 16 rows: where every unit finds a CU of its own, eight waves share its blocks; with more units two workgroups of four waves on every CU, so that
 // one's loads go on while the other one's waves meet (32 sequences of 100 to 500 positions over 32 heads 36.7 / 31.3 us, 200 of 20 to 300 over 8 heads
 // 41.7 / 32.9; the other way round 7B heads, 8000 positions 26.5 / 26.8, 70B heads, 120000 positions 88 / 100, 7B window of 16, 777 positions 13.3 / 15.8).
-// Heads of more than 128 elements and two tiles need the registers of a CU for four waves.
+// 17 to 32 rows run as two tiles, by as many waves as find their registers (eight instead of four, bf16 rows: 64 heads on 8, 4 rows, 2000 positions 27.2 / 22.7 us,
+// 40 sequences of 1000 54.9 / 48.2; the kernel for many rows 20.7 and 44.9 there, but 16 heads on 4 27.6 for 15.9), bf16 heads of more than 128 elements as many
+// rows (8 heads on 4 of 256, fp32 rows: 66.6 / 34.9), fp32 heads of 256, which would spill, as single tiles (88.7 / 53.1).
+static constexpr int pair_waves(int G, bool F32, int QP) { return G <= (F32 ? 2 : QP == 1 ? 4 : 3) ? 8 : 4; }
 template <int G, bool F32, int QP, int PP>
 static hipError_t launch(const PagedAttnArgs& a, hipStream_t st) {
     const int cus = fc_num_cus();
     if constexpr (!F32) {
-        if (a.r.R * a.g > 32) {
+        if (a.r.R * a.g > (G > 4 ? 16 : 32)) {
             constexpr int RT = 16 * many_groups(G, QP) * many_tiles(G);
             if constexpr (QP == 1)
                 if ((int64_t)a.r.B * a.c.Hkv * ((a.r.R * a.g + RT - 1) / RT) > cus) return launch_many<G, QP, 1>(a, 2 * cus, st);
             return launch_many<G, QP, 2>(a, cus, st);
         }
     }
-    if (a.r.R * a.g > 16) return launch_as<G, F32, 2, 4, QP, PP>(a, cus, st);
+    if constexpr (G <= 4 || (F32 && G < 8))
+        if (a.r.R * a.g > 16) return launch_as<G, F32, 2, pair_waves(G, F32, QP), QP, PP>(a, cus, st);
     if constexpr (G <= 4) {
         if ((int64_t)a.r.B * a.c.Hkv <= cus) return launch_as<G, F32, 1, 8, QP, PP>(a, cus, st);
         return launch_as<G, F32, 1, 4, QP, PP>(a, 2 * cus, st);

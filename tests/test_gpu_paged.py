@@ -108,6 +108,17 @@ CASES = [
     ([0], [300], 64, 2, 2, 128, "bf16", "f32", 1, 1),
     ([10], [30], 32, 2, 1, 96, "bf16", "f32", 10 ** 9, 10 ** 9),
     ([500], [2], 32, 4, 1, 128, "bf16", "f32", 40, 100),
+    # 17 to 32 rows of a K/V head
+    ([9, 700], [9, 14], 32, 4, 2, 64, "bf16", "f32", 0, 0),
+    ([9, 700], [9, 14], 32, 4, 2, 64, "bf16", "bf16", 90, 2),
+    ([9, 700], [9, 14], 32, 4, 2, 64, "f32", "f32", 0, 0),
+    ([31, 400], [5, 8], 64, 4, 1, 96, "bf16", "f32", 0, 0),
+    ([31, 400], [5, 8], 64, 4, 1, 96, "f32", "f32", 33, 1),
+    ([31, 1400], [17, 31], 64, 2, 2, 128, "bf16", "bf16", 0, 0),
+    ([31, 400], [17, 31], 64, 2, 2, 128, "f32", "f32", 0, 0),
+    ([31, 400], [17, 31], 64, 1, 1, 192, "f32", "f32", 0, 0),
+    ([31, 400], [5, 8], 64, 4, 1, 256, "bf16", "bf16", 0, 0),
+    ([31, 400], [5, 8], 64, 4, 1, 192, "bf16", "f32", 50, 3),
 ]
 
 
