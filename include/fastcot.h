@@ -297,7 +297,7 @@ int fastcot_attn_window_noalloc(const float* d_q, const void* d_k_cache, const v
  *
  * A pool (one for K, one for V) is [n_layers][n_pages][n_kv_heads][page_size / 32][32 * head_dim] elements of dtype: the blocks of
  * 32 positions of fastcot_kv_scatter's layout.  page_size: a power of two, 32 to 4096; head_dim: 32, 64, 96, 128, 192 or 256;
- * n_pages up to 2^24, max_seqs up to 4096, max_pages * page_size up to 2^30.
+ * n_pages up to 2^24, max_seqs up to 4096, max_pages * page_size up to 2^30, max_seqs * max_pages below 2^31, a pool below 2^60 elements.
  * table [max_seqs][max_pages]: page of positions i * page_size.. of a sequence, -1: none (no row sees those positions, and nothing is written
  * there).  len [max_seqs]: committed positions.  ref [n_pages]: sequences whose table names the page, 0: free.
  * All device memory is the caller's: pools (fastcot_paged_pool_bytes each, aligned to 16 bytes, contents arbitrary), table, len, ref (set by
@@ -346,8 +346,8 @@ int fastcot_paged_trim(const fastcot_paged* cache, int32_t count, const int32_t*
                        void* hip_stream);
 int fastcot_paged_free(const fastcot_paged* cache, int32_t count, const int32_t* d_seqs, int32_t* d_status, void* hip_stream);
 /* Moves the pages in use to the front of the pools: of U pages in use the i-th one (in ascending order) behind the first U places moves to the i-th
- * free place among them, and the tables follow.  d_used (device, nullable): U.  Afterwards a caller may give the rear of the pools back or
- * go on with a smaller n_pages (at least U). */
+ * free place among them, and the tables follow.  d_used (device, nullable): U.  Afterwards the first U pages of every layer are all that
+ * counts: a caller may copy them into smaller pools, or, with one layer, go on in these with a smaller n_pages (n_pages is the step between layers). */
 int fastcot_paged_compact(const fastcot_paged* cache, int32_t* d_used, void* d_scratch, void* hip_stream);
 
 /* The rows of a pass.  d_seqs: device, n_seqs sequence numbers, NULL: 0 .. n_seqs - 1 (a number out of range: its rows see nothing and are not

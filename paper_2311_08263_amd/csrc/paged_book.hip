@@ -363,7 +363,10 @@ static bool shape_ok(const fastcot_paged* c) {
     return c && c->n_layers >= 1 && c->n_layers <= 4096 && c->n_pages >= 1 && c->n_pages <= PG_MAX_PAGES && c->page_size >= 32 && c->page_size <= 4096 &&
            !(c->page_size & (c->page_size - 1)) && c->n_kv_heads >= 1 && c->n_kv_heads <= 4096 && head_dim_ok(c->head_dim) &&
            (c->dtype == FASTCOT_F32 || c->dtype == FASTCOT_BF16) && c->max_seqs >= 1 && c->max_seqs <= PG_MAX_SEQS && c->max_pages >= 1 &&
-           (int64_t)c->max_pages * c->page_size <= (int64_t)1 << 30 && (int64_t)c->n_layers * c->n_kv_heads * (c->page_size / 16) < (int64_t)1 << 31;
+           (int64_t)c->max_pages * c->page_size <= (int64_t)1 << 30 && (int64_t)c->n_layers * c->n_kv_heads * (c->page_size / 16) < (int64_t)1 << 31 &&
+           // (what an entry may need is summed in 32 bits, bytes of a pool in 64)
+           (int64_t)c->max_seqs * c->max_pages < (int64_t)1 << 31 &&
+           (double)c->n_layers * c->n_pages * c->n_kv_heads * c->page_size * c->head_dim < (double)((int64_t)1 << 60);
 }
 static size_t esz_of(const fastcot_paged* c) { return c->dtype == FASTCOT_BF16 ? 2 : 4; }
 static size_t page_bytes(const fastcot_paged* c) { return (size_t)c->n_kv_heads * c->page_size * c->head_dim * esz_of(c); }
@@ -502,8 +505,8 @@ extern "C" int fastcot_paged_write(const fastcot_paged* c, int32_t layer, const 
     if (row_stride % 8 || row_stride < (int64_t)c->n_kv_heads * c->head_dim) FAIL(FASTCOT_EINVAL, "%s: row stride below a row or no multiple of 8", name);
     char* kl = v.k + (size_t)layer * c->n_pages * page_bytes(c);
     char* vl = v.v + (size_t)layer * c->n_pages * page_bytes(c);
-    const int64_t gx = ((int64_t)(r.R + 31) / 32 + 1) * c->n_kv_heads;             // (rows may begin inside a block)
-    if (gx > 0x7FFFFFFF) FAIL(FASTCOT_ECAPACITY, "%s: too many rows of one sequence", name);
+    const int64_t gx = (((int64_t)r.R + 31) / 32 + 1) * c->n_kv_heads;             // (rows may begin inside a block)
+    if (r.R > 1 << 30 || gx > 0x7FFFFFFF) FAIL(FASTCOT_ECAPACITY, "%s: too many rows of one sequence", name);
     const dim3 grid((unsigned)gx, (unsigned)r.B);
     const size_t lds = 2 * 32 * (c->head_dim * esz_of(c) + 16);
     hipStream_t st = (hipStream_t)hip_stream;

@@ -35,7 +35,10 @@ def test_more_blocks_than_31_bits_count():
 
 
 BAD = [dict(n_layers=4096, n_kv_heads=4096, page_size=4096), dict(n_layers=0), dict(n_pages=0), dict(n_pages=(1 << 24) + 1), dict(page_size=16), dict(page_size=48), dict(page_size=8192), dict(n_kv_heads=0),
-       dict(head_dim=100), dict(head_dim=160), dict(dtype=2), dict(max_seqs=0), dict(max_seqs=4097), dict(max_pages=0), dict(max_pages=1 << 25)]
+       dict(head_dim=100), dict(head_dim=160), dict(dtype=2), dict(max_seqs=0), dict(max_seqs=4097), dict(max_pages=0), dict(max_pages=1 << 25),
+       # table entries past 31 bits, bytes of a pool past 64
+       dict(max_seqs=128, max_pages=1 << 24), dict(n_layers=512, n_pages=1 << 24, n_kv_heads=1024, page_size=4096, max_pages=1),
+       dict(n_layers=128, n_pages=1 << 24, n_kv_heads=4096, page_size=1024, head_dim=256, dtype=0, max_pages=1)]
 
 
 @pytest.mark.parametrize("bad", BAD, ids=str)
@@ -131,3 +134,4 @@ def test_write_arguments():
     refused(write(v=4104), b"16 bytes")
     refused(write(row=504), b"stride")
     refused(write(row=516), b"stride")
+    assert write(r=PagedRows(1, (1 << 30) + 1, (1 << 30) + 1, None, None)) == -3 and b"too many rows" in binding.lib().fastcot_last_error(None)
