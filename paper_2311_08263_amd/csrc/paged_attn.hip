@@ -359,7 +359,10 @@ __global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_at
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedDeal deal;
     PagedPart part;
-    if (!pg_deal<RT>(a, tiles, blockIdx.x, gridDim.x, deal, part)) return;
+    // fp32 caches run many rows here too: consecutive shares go to one XCD, whose L2 holds the blocks that units of one K/V head find after each other (they are
+    // loaded to stay there: 1695, 21 and 2001 rows of 7B heads 1205 / 886 us, 1000 rows of 8 heads on 4 of 256 164 / 110)
+    const int worker = F32 && !(gridDim.x & 7) ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+    if (!pg_deal<RT>(a, tiles, worker, gridDim.x, deal, part)) return;
   do {
     if (part.len <= 0) continue;                               // (a share that ends in front of the unit's first block)
     const int kvh = part.kvh, first = part.first, nrows = part.rows, seq = part.seq, n = part.n;
@@ -425,11 +428,11 @@ __global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_at
 #pragma unroll
         for (int f = 0; f < 2 * G; ++f)
 #pragma unroll
-            for (int w = 0; w < FW; ++w) kf[f][w] = __builtin_nontemporal_load(kp + f * 64 * FW + w);
+            for (int w = 0; w < FW; ++w) kf[f][w] = F32 ? kp[f * 64 * FW + w] : __builtin_nontemporal_load(kp + f * 64 * FW + w);
 #pragma unroll
         for (int f = 0; f < NV; ++f)
 #pragma unroll
-            for (int w = 0; w < FW; ++w) vf[f][w] = __builtin_nontemporal_load(vp + f * 64 * FW + w);
+            for (int w = 0; w < FW; ++w) vf[f][w] = F32 ? vp[f * 64 * FW + w] : __builtin_nontemporal_load(vp + f * 64 * FW + w);
         // every row sees all 32 positions
         const bool whole = kb + 31 <= p0 && (!a.window || kb > p1 - a.window || kb + 31 < a.sinks);
         bool odd = false;                                      // V is not finite where some rows see it and others do not
@@ -533,7 +536,7 @@ __global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_at
     }
     __syncthreads();
     const bool shared = part.len < part.blocks;
-    float* mine = a.part + (size_t)(2 * blockIdx.x + (part.off == 0)) * RT * (Dh + 2);
+    float* mine = a.part + (size_t)(2 * worker + (part.off == 0)) * RT * (Dh + 2);
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int x = row0 + 16 * qt + lm;
