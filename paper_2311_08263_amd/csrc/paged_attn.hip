@@ -424,6 +424,8 @@ __global__ __launch_bounds__(NW * 64, QT == 1 && G <= 4 ? 2 : 1) void k_paged_at
         constexpr int FW = F32 ? 2 : 1;                        // 16-byte words of a lane's eight values
         const u32x4_t* kp = (const u32x4_t*)(a.kl + at * (F32 ? 4 : 2)) + lane * FW;
         const u32x4_t* vp = (const u32x4_t*)(a.vl + at * (F32 ? 4 : 2)) + lane * FW;
+        // (bf16 blocks go past the caches: 48 sequences of 60 to 8100 positions 264 us, 297 if not.  Of fp32 ones a lane takes its 32 bytes in two loads, which
+        // share their lines: one token of 20 sequences of 8000 positions 864, past the caches 904)
         u32x4_t kf[2 * G][FW], vf[NV][FW];
 #pragma unroll
         for (int f = 0; f < 2 * G; ++f)
